@@ -1,0 +1,488 @@
+"""Single operators of serving beyond a plain decode step, as measurable cases.
+
+Rotary tables for long contexts, rotation with cache append at given positions, decode attention for a batch that
+shares a prefix, decode attention that accumulates the weight of every cached token, and eviction by that weight.
+Head shapes are those of ``workloads`` (tiny, 7B, 13B, 8B-GQA). ``run`` computes the operators in plain torch, or
+with the library's kernels when ``own`` is set; ``exact`` computes them in 64 bits from their definitions.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+BLOCK = 16  # tokens per KV block
+HEADS = {"tiny": (4, 4, 64), "7b": (32, 32, 128), "13b": (40, 40, 128), "8b": (32, 8, 128)}  # query heads, kv heads, head dim
+BASE = {"tiny": 10000.0, "7b": 10000.0, "13b": 10000.0, "8b": 500000.0}
+
+
+def listed():
+    return [
+        # The tables of a stage of the tiny model: next to nothing but a launch.
+        dict(name="tables-tiny-1k", kind="tables", model="tiny", max_pos=1024, rot=64, scaling="plain", factor=1.0, original=1024),
+        # A model trained on 8192 positions served with 131072: the largest tables.
+        dict(name="tables-8b-128k", kind="tables", model="8b", max_pos=131072, rot=128, scaling="bands", factor=8.0, original=8192),
+        # One decode step of 16 users after evictions, two rows of the batch empty: positions are not slots.
+        dict(name="rope-8b-decode16", kind="rope", model="8b", tokens=16, rot=128, layout="half", max_pos=8192, pad=2, keys=False),
+        # A full prefill call: keys to the cache and to the packed rows that the prompt's attention reads.
+        dict(name="rope-8b-prefill8192", kind="rope", model="8b", tokens=8192, rot=128, layout="half", max_pos=16384, pad=0, keys=True),
+        # An odd number of tokens, interleaved pairs on half of each head, many heads.
+        dict(name="rope-13b-partial1531", kind="rope", model="13b", tokens=1531, rot=64, layout="interleaved", max_pos=4096, pad=3, keys=True),
+        # A short system prompt and first answers: latency is all there is.
+        dict(name="shared-tiny-b3", kind="shared", model="tiny", seqs=3, prefix=77, lo=0, hi=20),
+        # Many users of one assistant: a long system prompt, short conversations.
+        dict(name="shared-8b-b32-8k", kind="shared", model="8b", seqs=32, prefix=8192, lo=64, hi=512),
+        # Questions about one document by one head per kv head, odd sizes.
+        dict(name="shared-13b-b24-2011", kind="shared", model="13b", seqs=24, prefix=2011, lo=1, hi=300),
+        # One user's cache under a budget: the weights of a single sequence.
+        dict(name="weights-7b-b1", kind="weights", model="7b", seqs=1, prefix=0, lo=1100, hi=1100),
+        # A batch under a budget behind a shared prompt, ragged caches.
+        dict(name="weights-8b-b24", kind="weights", model="8b", seqs=24, prefix=1000, lo=512, hi=4096),
+        # Steady state of a budget of 2048: every cache a little over it.
+        dict(name="evict-8b-b32", kind="evict", model="8b", seqs=32, lo=2049, hi=2176, keep=2048, sinks=4, recent=256),
+        # Two long prompts cut down to the budget after prefill.
+        dict(name="evict-7b-b2-prompt", kind="evict", model="7b", seqs=2, lo=11000, hi=12000, keep=2048, sinks=4, recent=64),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case: tables of 64 to 131072 positions, 1 to 8192 rotated tokens, prefixes of 0 to 8192 and own caches of 0 to 4096 tokens in
+    1 to 64 sequences, evictions from caches of 1 to 12000 tokens."""
+    kind = rng.choices(["tables", "rope", "shared", "weights", "evict"], [1, 2, 4, 3, 3])[0]
+    model = rng.choice(list(HEADS))
+    nh, nkv, d = HEADS[model]
+    if kind == "tables":
+        n = _log_int(rng, 64, 131072)
+        scaling = rng.choice(["plain", "linear", "ntk", "bands", "yarn"])
+        factor = 1.0 if scaling == "plain" else rng.choice([1.5, 2.0, 4.0, 8.0, 32.0])
+        return dict(kind=kind, model=model, max_pos=n, rot=rng.choice([16, 32, 48, 64, 80, 96, 128]), scaling=scaling, factor=factor,
+                    original=max(16, int(n / factor)))
+    if kind == "rope":
+        n = _log_int(rng, 1, 8192)
+        return dict(kind=kind, model=model, tokens=n, rot=rng.choice([16, 32, d // 2, d // 4 * 3, d, d]), layout=rng.choice(["half", "interleaved"]),
+                    max_pos=_log_int(rng, 1024, 32768), pad=min(n // 3, rng.randint(0, 3)), keys=n > 64)
+    if kind == "evict":
+        n = _log_int(rng, 1, 64)
+        hi = _log_int(rng, 16, min(12000, (200000 if nkv == 8 else 40000) // n))
+        keep = rng.randint(1, max(1, int(hi * 1.1)))
+        recent = rng.randint(0, keep // 2)
+        return dict(kind=kind, model=model, seqs=n, lo=rng.randint(hi // 4, hi), hi=hi, keep=keep, sinks=rng.randint(0, min(8, keep - recent)), recent=recent)
+    n = _log_int(rng, 1, 64 if kind == "shared" else 24)
+    prefix = _log_int(rng, 16, 8192) if kind == "shared" or rng.random() < 0.5 else 0
+    hi = _log_int(rng, 1 if prefix else 16, min(4096, (60000 if nkv == 8 else 15000) // n))
+    return dict(kind=kind, model=model, seqs=n, prefix=prefix, lo=rng.randint(0 if prefix else 1, hi), hi=hi)
+
+
+# ------------------------------------------------------------------ inputs
+
+
+def lengths(case):
+    """Cached tokens of the case's sequences."""
+    r = random.Random("%d %d %d" % (case["seqs"], case["lo"], case["hi"]))
+    return [r.randint(case["lo"], case["hi"]) for _ in range(case["seqs"])]
+
+
+def _gen(seed, what):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(random.Random("%d %s" % (seed, what)).getrandbits(48))
+    return g
+
+
+def _normal(seed, what, shape, std=1.0):
+    x = torch.empty(shape, dtype=torch.float32, device=DEV).normal_(0.0, std, generator=_gen(seed, what))
+    return x.to(torch.bfloat16)
+
+
+def _i32(x):
+    return torch.as_tensor(np.asarray(x, np.int32), device=DEV)
+
+
+def _weights(seed, what, shape):
+    """Accumulated attention weights: most tokens little, a few much, some none at all (ties)."""
+    g = _gen(seed, what)
+    x = torch.empty(shape, dtype=torch.float32, device=DEV).normal_(0.0, 2.0, generator=g).exp_() * 0.01
+    return torch.where(torch.rand(shape, device=DEV, generator=g) < 0.05, torch.zeros_like(x), x)
+
+
+def _pages(seed, lens, width):
+    """A shuffled pool's pages for caches of up to `width` pages each: table [n][width], pages in the pool. Every entry names a page of its own."""
+    n = len(lens) * width
+    perm = torch.randperm(n + 3, device=DEV, generator=_gen(seed, "pages"))[:n]
+    return perm.to(torch.int32).view(len(lens), width), n + 3
+
+
+def frequencies(case, base):
+    """Angle per position of every pair, in 64 bits, and the magnitude of the rotation."""
+    rot, f, kind, n = case["rot"], case["factor"], case["scaling"], case["original"]
+    i = np.arange(rot // 2, dtype=np.float64)
+    w = base ** (-2.0 * i / rot)
+    if kind == "linear":
+        return w / f, 1.0
+    if kind == "ntk":
+        return (base * f ** (rot / (rot - 2.0))) ** (-2.0 * i / rot), 1.0
+    if kind == "bands":  # fewer than 1 turn in the original context: stretched; more than 4: as they were
+        s = np.clip((n * w / (2 * math.pi) - 1.0) / 3.0, 0.0, 1.0)
+        return (1.0 - s) * w / f + s * w, 1.0
+    if kind == "yarn":  # the same by pair index, between 32 turns and 1
+        at = lambda turns: rot * math.log(n / (2 * math.pi * turns)) / (2 * math.log(base))  # noqa: E731
+        a, b = max(0.0, math.floor(at(32.0))), min(rot - 1.0, math.ceil(at(1.0)))
+        r = np.clip((i - a) / max(b - a, 1e-3), 0.0, 1.0)
+        return r * w / f + (1.0 - r) * w, 0.1 * math.log(f) + 1.0
+    return w, 1.0
+
+
+def prepare(case, seed):
+    nh, nkv, d = HEADS[case["model"]]
+    s = dict(case=case, nh=nh, nkv=nkv, d=d)
+    if case["kind"] == "tables":
+        shape = (case["max_pos"], case["rot"] // 2)
+        # another base for every seed, as models have, whole numbers below 2^24
+        return s | dict(base=float(round(BASE[case["model"]] * random.Random("%d base" % seed).uniform(0.5, 2.0))),
+                        cos=torch.empty(shape, dtype=torch.float32, device=DEV), sin=torch.empty(shape, dtype=torch.float32, device=DEV))
+    if case["kind"] == "rope":
+        t, n = case["tokens"], case["max_pos"]
+        r = random.Random("%d rope" % seed)
+        if case["keys"]:  # packed chunks of prompts, each somewhere in its sequence
+            pos = []
+            while len(pos) < t:
+                m = min(t - len(pos), r.randint(1, max(1, min(t, n))))
+                at = r.randint(0, n - m) if m < n else 0
+                pos += range(at, at + min(m, n))
+        else:
+            pos = [r.randrange(n) for _ in range(t)]
+        for i in r.sample(range(t), case["pad"]):
+            pos[i] = -1
+        pos = np.array(pos, np.int32)
+        pages = -(-t // BLOCK)
+        order = np.random.RandomState(r.getrandbits(31)).permutation(pages)
+        slot = np.where(pos >= 0, order[np.arange(t) // BLOCK] * BLOCK + np.arange(t) % BLOCK, -1)
+        if not case["keys"]:  # one new token in each sequence's last page
+            pages = t
+            slot = np.where(pos >= 0, np.random.RandomState(r.getrandbits(31)).permutation(t) * BLOCK + np.arange(t) * 5 % BLOCK, -1)
+        ang = torch.arange(n, dtype=torch.float64, device=DEV)[:, None] * torch.as_tensor(frequencies(case | dict(scaling="plain", factor=1.0, original=n), BASE[case["model"]])[0], device=DEV)
+        return s | dict(qkv=_normal(seed, "qkv", (t, (nh + 2 * nkv) * d)), pos=_i32(pos), slot=_i32(slot), cos=ang.cos().float(), sin=ang.sin().float(),
+                        pool=_normal(seed, "pool", (pages + 1, 2, nkv, BLOCK, d)), q_out=torch.zeros((t, nh * d), dtype=torch.bfloat16, device=DEV),
+                        k_out=torch.zeros((t, nkv * d), dtype=torch.bfloat16, device=DEV) if case["keys"] else None)
+    lens = lengths(case)
+    width = -(-max(max(lens), 1) // BLOCK)
+    table, pages = _pages(seed, lens, width)
+    s |= dict(table=table, ctx=_i32(lens), max_ctx=max(lens), width=width, n_seqs=len(lens))
+    if case["kind"] == "evict":
+        most = max(lens)
+        kept = max(1, min(case["keep"], most))
+        # positions: caches that were evicted before are in no order and have gaps
+        gaps = torch.rand((len(lens), nkv, most), device=DEV, generator=_gen(seed, "gaps")).mul(3).int() + 1
+        pos = gaps.cumsum(2, dtype=torch.int32) - gaps[:, :, :1]
+        seen = pos.gather(2, (s["ctx"].long() - 1).clamp(min=0)[:, None, None].expand(-1, nkv, 1)).amax((1, 2)).to(torch.int32) + 1
+        swap = torch.rand((len(lens), nkv, most), device=DEV, generator=_gen(seed, "swap"))
+        half = max(1, min(lens) // 2)
+        at = torch.argsort(swap[:, :, :half], dim=2)
+        pos = torch.cat([pos[:, :, :half].gather(2, at), pos[:, :, half:]], 2).contiguous()
+        return s | dict(pool=_normal(seed, "pool", (pages, 2, nkv, BLOCK, d)), acc=_weights(seed, "acc", (len(lens), nkv, most)), pos=pos, seen=seen,
+                        acc_out=torch.zeros((len(lens), nkv, kept), dtype=torch.float32, device=DEV),
+                        pos_out=torch.full((len(lens), nkv, kept), -1, dtype=torch.int32, device=DEV), ctx_out=torch.zeros(len(lens), dtype=torch.int32, device=DEV))
+    shared = -(-case["prefix"] // BLOCK)
+    prefix = torch.arange(pages, pages + shared, dtype=torch.int32, device=DEV)[torch.randperm(shared, device=DEV, generator=_gen(seed, "prefix"))]
+    n, pages = len(lens), pages + shared
+    s |= dict(q=_normal(seed, "q", (n, nh * d)), pool=_normal(seed, "pool", (pages, 2, nkv, BLOCK, d)), prefix=prefix.contiguous(),
+              out=torch.zeros((n, nh * d), dtype=torch.bfloat16, device=DEV))
+    if case["kind"] == "weights":
+        most = max(lens)
+        s |= dict(acc=_weights(seed, "acc", (n, nkv, most)), acc_out=torch.zeros((n, nkv, most), dtype=torch.float32, device=DEV),
+                  pos=torch.arange(most, dtype=torch.int32, device=DEV).expand(n, nkv, most).contiguous(), seen=s["ctx"] * 2 + 5)
+    return s
+
+
+DECAY = 0.96875
+
+
+# ------------------------------------------------------------- plain forms
+
+
+def _plain_tables(s):
+    w, m = frequencies(s["case"], s["base"])
+    ang = torch.arange(s["case"]["max_pos"], dtype=torch.float64, device=DEV)[:, None] * torch.as_tensor(w, device=DEV)
+    s["cos"].copy_(ang.cos() * m)
+    s["sin"].copy_(ang.sin() * m)
+    return s["cos"], s["sin"]
+
+
+def _plain_rope(s):
+    c, nh, nkv, d = s["case"], s["nh"], s["nkv"], s["d"]
+    t, rot = c["tokens"], c["rot"]
+    x = s["qkv"].view(t, nh + 2 * nkv, d)
+    real = (s["pos"] >= 0)[:, None, None]
+    at = s["pos"].clamp(min=0).long()
+    cos, sin = s["cos"][at][:, None], s["sin"][at][:, None]
+    y = x[:, :nh + nkv].float()
+    if c["layout"] == "half":
+        a, b = y[:, :, :rot // 2], y[:, :, rot // 2:rot]
+        y = torch.cat([a * cos - b * sin, b * cos + a * sin, y[:, :, rot:]], 2)
+    else:
+        a, b = y[:, :, 0:rot:2], y[:, :, 1:rot:2]
+        y = torch.cat([torch.stack([a * cos - b * sin, b * cos + a * sin], 3).flatten(2), y[:, :, rot:]], 2)
+    y = y.to(torch.bfloat16)
+    s["q_out"].copy_(torch.where(real, y[:, :nh], s["q_out"].view(t, nh, d)).view(t, -1))
+    if c["keys"]:
+        s["k_out"].copy_(torch.where(real, y[:, nh:], s["k_out"].view(t, nkv, d)).view(t, -1))
+    pool = s["pool"]
+    slot = torch.where(s["slot"] >= 0, s["slot"], (pool.shape[0] - 1) * BLOCK).long()  # empty rows: the spare page gets what it has
+    page, off = slot // BLOCK, slot % BLOCK
+    pool[page, 0, :, off] = torch.where(real, y[:, nh:], pool[page, 0, :, off])
+    pool[page, 1, :, off] = torch.where(real, x[:, nh + nkv:], pool[page, 1, :, off])
+    return s["q_out"], s["k_out"], pool
+
+
+def _plain_attention(s):
+    """Output and, for every own token, the probabilities of the query heads."""
+    c, nh, nkv, d, n = s["case"], s["nh"], s["nkv"], s["d"], s["n_seqs"]
+    g, p, pool = nh // nkv, c["prefix"], s["pool"]
+    q = s["q"].view(n, nkv, g, d).float() / math.sqrt(d)
+    kv = pool[s["prefix"].long()].permute(1, 2, 0, 3, 4).reshape(2, nkv, -1, d)[:, :, :p].float()
+    own_kv = pool[s["table"].long()].permute(2, 0, 3, 1, 4, 5).reshape(2, n, nkv, -1, d).float()
+    rows = q.transpose(0, 1).reshape(nkv, n * g, d).contiguous()
+    shared = torch.matmul(rows, kv[0].transpose(1, 2).contiguous()).view(nkv, n, g, p).transpose(0, 1)
+    mine = torch.matmul(q, own_kv[0].transpose(2, 3).contiguous())
+    valid = torch.arange(mine.shape[3], device=DEV) < s["ctx"][:, None, None, None]
+    x = torch.cat([shared, mine.masked_fill(~valid, -math.inf)], 3)
+    m = x.amax(3, keepdim=True)
+    e = torch.exp(x - torch.where(m == -math.inf, torch.zeros_like(m), m))
+    prob = e / e.sum(3, keepdim=True).clamp(min=1e-38)
+    o = torch.matmul(prob[..., :p].transpose(0, 1).reshape(nkv, n * g, p).contiguous(), kv[1].contiguous()).view(nkv, n, g, d).transpose(0, 1)
+    o = o + torch.matmul(prob[..., p:], own_kv[1])
+    s["out"].copy_(o.reshape(n, nh * d))
+    return prob[..., p:]
+
+
+def _plain_shared(s):
+    _plain_attention(s)
+    return s["out"]
+
+
+def _plain_weights(s):
+    prob = _plain_attention(s).sum(2)[:, :, :s["max_ctx"]]
+    t = torch.arange(s["max_ctx"], device=DEV)
+    ctx = s["ctx"][:, None, None]
+    s["acc_out"].copy_(torch.where(t < ctx, torch.where(t == ctx - 1, prob, s["acc"] * DECAY + prob), s["acc_out"]))
+    s["pos"].copy_(torch.where(t == ctx - 1, s["seen"][:, None, None] - 1, s["pos"]))
+    return s["out"], s["acc_out"], s["pos"]
+
+
+def _plain_evict(s):
+    c, nkv, n, most = s["case"], s["nkv"], s["n_seqs"], s["max_ctx"]
+    keep, kept = c["keep"], s["acc_out"].shape[2]
+    ctx, t = s["ctx"][:, None, None], torch.arange(most, device=DEV)
+    valid = t < ctx
+    forced = (s["pos"] < c["sinks"]) | (s["pos"] >= s["seen"][:, None, None] - c["recent"])
+    # rank 0 stays first: protected, then by weight, then the lower slot; no cached token last
+    order = torch.argsort(torch.where(valid, torch.where(forced, math.inf, s["acc"]), -math.inf), dim=2, descending=True, stable=True)
+    rank = torch.empty_like(order).scatter_(2, order, t.expand_as(order))
+    stays = valid & (rank < keep)
+    hole, comes = (~stays) & (t < torch.clamp(ctx, max=keep)), stays & (t >= keep)
+    # the j-th hole takes the j-th token that stays at or past `keep`
+    source = torch.argsort((~comes).int(), dim=2, stable=True)
+    source = torch.where(hole, source.gather(2, (hole.int().cumsum(2) - 1).clamp(min=0)), t)[:, :, :kept]
+    there = valid[:, :, :kept].expand(n, nkv, kept)
+    s["acc_out"].copy_(torch.where(there, s["acc"].gather(2, source), s["acc_out"]))
+    s["pos_out"].copy_(torch.where(there, s["pos"].gather(2, source), s["pos_out"]))
+    s["ctx_out"].copy_(s["ctx"].clamp(max=keep))
+    pool, table, head = s["pool"], s["table"].long(), torch.arange(nkv, device=DEV)[None, :, None]
+    seq = torch.arange(n, device=DEV)[:, None, None]
+    here = t[:kept].expand(n, nkv, kept)
+    page, off = table[seq, here // BLOCK], here % BLOCK
+    from_page, from_off = table[seq, source // BLOCK], source % BLOCK
+    pool[page, 0, head, off] = pool[from_page, 0, head, from_off]
+    pool[page, 1, head, off] = pool[from_page, 1, head, from_off]
+    return pool, s["acc_out"], s["pos_out"], s["ctx_out"]
+
+
+# ---------------------------------------------------------- the library's
+
+
+def _p(x):
+    return 0 if x is None else x.data_ptr()
+
+
+def _workspace(s, size):
+    """Device memory that the calls of one kind share, as a program keeps it."""
+    if "ws" not in s:
+        s["ws"] = torch.empty(max(size(), 16), dtype=torch.uint8, device=DEV)
+    return s["ws"].data_ptr(), s["ws"].numel()
+
+
+def _own_tables(hs, s, stream):
+    c = s["case"]
+    scaling = hs.rope_scaling(c["scaling"], factor=c["factor"], original_ctx=c["original"])
+    hs.hs_k_rope_tables(_p(s["cos"]), _p(s["sin"]), c["max_pos"], c["rot"], s["base"], scaling, stream)
+    return s["cos"], s["sin"]
+
+
+def _own_rope(hs, s, stream):
+    c, nh, nkv, d = s["case"], s["nh"], s["nkv"], s["d"]
+    hs.hs_k_rope_kv(_p(s["qkv"]), (nh + 2 * nkv) * d, _p(s["pos"]), _p(s["slot"]), _p(s["cos"]), _p(s["sin"]), c["max_pos"], c["rot"], c["layout"],
+                    _p(s["q_out"]), nh * d, _p(s["k_out"]), nkv * d, _p(s["pool"]), s["pool"].shape[0], c["tokens"], nh, nkv, d, stream)
+    return s["q_out"], s["k_out"], s["pool"]
+
+
+def _own_shared(hs, s, stream):
+    c, nh, nkv, d, n = s["case"], s["nh"], s["nkv"], s["d"], s["n_seqs"]
+    ws = _workspace(s, lambda: hs.hs_k_attn_decode_shared_ws(n, nh, nkv, d, c["prefix"], s["max_ctx"]))
+    hs.hs_k_attn_decode_shared(_p(s["q"]), nh * d, _p(s["pool"]), s["pool"].shape[0], _p(s["prefix"]), c["prefix"], _p(s["table"]), _p(s["ctx"]),
+                               _p(s["out"]), nh * d, n, nh, nkv, d, s["width"], s["max_ctx"], *ws, stream)
+    return s["out"]
+
+
+def _own_weights(hs, s, stream):
+    c, nh, nkv, d, n = s["case"], s["nh"], s["nkv"], s["d"], s["n_seqs"]
+    ws = _workspace(s, lambda: hs.hs_k_attn_decode_weights_ws(n, nh, nkv, d, c["prefix"], s["max_ctx"]))
+    hs.hs_k_attn_decode_weights(_p(s["q"]), nh * d, _p(s["pool"]), s["pool"].shape[0], _p(s["prefix"]), c["prefix"], _p(s["table"]), _p(s["ctx"]),
+                                _p(s["out"]), nh * d, _p(s["acc"]), _p(s["acc_out"]), s["max_ctx"], DECAY, _p(s["pos"]), _p(s["seen"]),
+                                n, nh, nkv, d, s["width"], s["max_ctx"], *ws, stream)
+    return s["out"], s["acc_out"], s["pos"]
+
+
+def _own_evict(hs, s, stream):
+    c, nkv, d, n = s["case"], s["nkv"], s["d"], s["n_seqs"]
+    ws = _workspace(s, lambda: hs.hs_k_kv_evict_ws(n, nkv, c["keep"], s["max_ctx"]))
+    hs.hs_k_kv_evict(_p(s["pool"]), s["pool"].shape[0], _p(s["table"]), _p(s["ctx"]), _p(s["seen"]), _p(s["acc"]), _p(s["pos"]), s["max_ctx"],
+                     _p(s["acc_out"]), _p(s["pos_out"]), s["acc_out"].shape[2], _p(s["ctx_out"]), c["keep"], c["sinks"], c["recent"],
+                     n, nkv, d, s["width"], s["max_ctx"], *ws, stream)
+    return s["pool"], s["acc_out"], s["pos_out"], s["ctx_out"]
+
+
+PLAIN = dict(tables=_plain_tables, rope=_plain_rope, shared=_plain_shared, weights=_plain_weights, evict=_plain_evict)
+OWN = dict(tables=_own_tables, rope=_own_rope, shared=_own_shared, weights=_own_weights, evict=_own_evict)
+
+
+def run(state):
+    if own:
+        from paper_2502_15524_amd import hs
+        return OWN[state["case"]["kind"]](hs, state, torch.cuda.current_stream().cuda_stream)
+    return PLAIN[state["case"]["kind"]](state)
+
+
+def work(case):
+    nh, nkv, d = HEADS[case["model"]]
+    if case["kind"] == "tables":
+        n = case["max_pos"] * (case["rot"] // 2)
+        return {"bytes": 8.0 * n, "flops": 3.0 * n}
+    if case["kind"] == "rope":
+        t = case["tokens"] - case["pad"]
+        heads = (nh + 2 * nkv) + nh + 2 * nkv + (nkv if case["keys"] else 0)  # read; q out; append; k out
+        return {"bytes": t * (heads * d * 2.0 + 8) + 4.0 * case["rot"] * min(t, case["max_pos"]), "flops": 3.0 * t * (nh + nkv) * case["rot"]}
+    lens = lengths(case)
+    if case["kind"] == "evict":
+        gone = [max(0, x - case["keep"]) for x in lens]
+        # the weights and positions of every token, what stays of them, and the rows of the tokens that stay past the budget
+        moved = sum(min(g, case["keep"]) * 0.5 if g else 0 for g in gone)
+        return {"bytes": nkv * (8.0 * sum(lens) + 8.0 * sum(min(x, case["keep"]) for x in lens) + 8.0 * d * moved), "flops": 0.0}
+    n = len(lens)
+    by = 4.0 * nkv * d * (case["prefix"] + sum(lens)) + 4.0 * n * nh * d
+    if case["kind"] == "weights":
+        by += 8.0 * nkv * sum(lens)
+    return {"bytes": by, "flops": 4.0 * nh * d * (n * case["prefix"] + sum(lens))}
+
+
+# ------------------------------------------------------------------- exact
+
+
+def _exact_rope(s):
+    c, nh, nkv, d = s["case"], s["nh"], s["nkv"], s["d"]
+    t, rot = c["tokens"], c["rot"]
+    half = rot // 2
+    pos, slot = s["pos"].cpu().numpy(), s["slot"].cpu().numpy()
+    live = torch.as_tensor(np.nonzero(pos >= 0)[0], device=DEV)
+    rows = s["qkv"].double().view(t, -1, d)[live]
+    turn = torch.complex(s["cos"].double(), s["sin"].double())[torch.as_tensor(pos[pos >= 0].astype(np.int64), device=DEV)][:, None]
+    i = torch.arange(half, device=DEV)
+    first, second = (i, i + half) if c["layout"] == "half" else (2 * i, 2 * i + 1)
+    qk = rows[:, :nh + nkv].clone()
+    z = torch.complex(qk[:, :, first], qk[:, :, second]) * turn
+    qk[:, :, first], qk[:, :, second] = z.real, z.imag
+    q_out = torch.zeros((t, nh * d), dtype=torch.float64, device=DEV)
+    q_out[live] = qk[:, :nh].reshape(len(live), -1)
+    k_out = None
+    if c["keys"]:
+        k_out = torch.zeros((t, nkv * d), dtype=torch.float64, device=DEV)
+        k_out[live] = qk[:, nh:].reshape(len(live), -1)
+    pool = s["pool"].double().transpose(2, 3).contiguous()  # [page][k, v][offset][head]
+    at = torch.as_tensor(slot[pos >= 0].astype(np.int64), device=DEV)
+    pool[at // BLOCK, 0, at % BLOCK] = qk[:, nh:]
+    pool[at // BLOCK, 1, at % BLOCK] = rows[:, nh + nkv:]
+    return q_out, k_out, pool.transpose(2, 3).contiguous()
+
+
+def _exact_attention(s):
+    c, nh, nkv, d = s["case"], s["nh"], s["nkv"], s["d"]
+    g = nh // nkv
+    lens, table = lengths(c), s["table"].long()
+
+    def rows(pages, n):  # keys, values [kv head][n][d]
+        kv = s["pool"][pages].double()
+        return [kv[:, j].transpose(0, 1).reshape(nkv, -1, d)[:, :n] for j in (0, 1)]
+
+    shared = rows(s["prefix"].long(), c["prefix"])
+    out = torch.zeros((len(lens), nh * d), dtype=torch.float64, device=DEV)
+    new = None
+    if c["kind"] == "weights":
+        new = torch.zeros((len(lens), nkv, s["max_ctx"]), dtype=torch.float64, device=DEV)
+    for b, n in enumerate(lens):
+        mine = rows(table[b], n)
+        k, v = (torch.cat([x, y], 1) for x, y in zip(shared, mine))
+        p = torch.softmax(s["q"][b].double().view(nkv, g, d) @ k.transpose(1, 2).contiguous() * d ** -0.5, 2)
+        out[b] = (p @ v).reshape(-1)
+        if new is not None and n:
+            new[b, :, :n] = p[:, :, c["prefix"]:].sum(1)
+            new[b, :, :n - 1] += DECAY * s["acc"][b, :, :n - 1].double()
+            s["pos"][b, :, n - 1] = s["seen"][b] - 1
+    return out if new is None else (out, new, s["pos"])
+
+
+def _exact_evict(s):
+    c, nkv = s["case"], s["nkv"]
+    keep, lens = c["keep"], lengths(c)
+    acc, pos, seen = s["acc"].double().cpu().numpy(), s["pos"].cpu().numpy(), s["seen"].cpu().numpy()
+    acc_out, pos_out = np.zeros(s["acc_out"].shape), np.full(s["pos_out"].shape, -1, np.int32)
+    to, come = [], []
+    table = s["table"].cpu().numpy().astype(np.int64)
+    for b, n in enumerate(lens):
+        for h in range(nkv):
+            a, p = acc[b, h, :n], pos[b, h, :n]
+            held = (p < c["sinks"]) | (p >= seen[b] - c["recent"])
+            best = np.lexsort((np.arange(n), -a, ~held))[:keep]
+            slots = np.arange(min(n, keep))
+            free = np.setdiff1d(slots, best)
+            late = np.sort(best[best >= keep])
+            slots[free] = late
+            acc_out[b, h, :len(slots)], pos_out[b, h, :len(slots)] = a[slots], p[slots]
+            to.append(np.stack([table[b, free // BLOCK], np.full(len(free), h), free % BLOCK]))
+            come.append(np.stack([table[b, late // BLOCK], np.full(len(late), h), late % BLOCK]))
+    to, come = (torch.as_tensor(np.concatenate(x, 1), device=DEV) for x in (to, come))
+    pool = s["pool"].clone()
+    for j in (0, 1):
+        pool[to[0], j, to[1], to[2]] = s["pool"][come[0], j, come[1], come[2]]
+    return pool, torch.as_tensor(acc_out), torch.as_tensor(pos_out), torch.as_tensor(np.minimum(lens, keep).astype(np.int32))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "rope":
+        return _exact_rope(s)
+    if case["kind"] == "evict":
+        return _exact_evict(s)
+    if case["kind"] != "tables":
+        return _exact_attention(s)
+    w, m = frequencies(case, s["base"])
+    # turns in more than 64 bits, whole ones taken off before the angle is rounded
+    turns = np.arange(case["max_pos"], dtype=np.longdouble)[:, None] * (w.astype(np.longdouble) / (2 * np.arctan2(np.longdouble(0), np.longdouble(-1))))
+    ang = ((turns - np.rint(turns)) * (2 * np.arctan2(np.longdouble(0), np.longdouble(-1)))).astype(np.float64)
+    return torch.as_tensor(np.cos(ang) * m), torch.as_tensor(np.sin(ang) * m)
