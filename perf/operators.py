@@ -458,7 +458,7 @@ def _exact_evict(s):
         for h in range(nkv):
             a, p = acc[b, h, :n], pos[b, h, :n]
             held = (p < c["sinks"]) | (p >= seen[b] - c["recent"])
-            best = np.lexsort((np.arange(n), -a, ~held))[:keep]
+            best = np.lexsort((np.arange(n), np.where(held, 0.0, -a), ~held))[:keep]
             slots = np.arange(min(n, keep))
             free = np.setdiff1d(slots, best)
             late = np.sort(best[best >= keep])
