@@ -55,7 +55,7 @@ def _log_int(rng, lo, hi):
 
 
 def draw(rng):
-    """One more case: tables of 64 to 131072 positions, 1 to 8192 rotated tokens, prefixes of 0 to 8192 and own caches of 0 to 4096 tokens in
+    """One more case: tables of 64 to 131072 positions, 1 to 8192 rotated tokens (to 3000 of 32 and more kv heads), prefixes of 0 to 8192 and own caches of 0 to 4096 tokens in
     1 to 64 sequences, evictions from caches of 1 to 12000 tokens."""
     kind = rng.choices(["tables", "rope", "shared", "weights", "evict"], [1, 2, 4, 3, 3])[0]
     model = rng.choice(list(HEADS))
@@ -67,7 +67,7 @@ def draw(rng):
         return dict(kind=kind, model=model, max_pos=n, rot=rng.choice([16, 32, 48, 64, 80, 96, 128]), scaling=scaling, factor=factor,
                     original=max(16, int(n / factor)))
     if kind == "rope":
-        n = _log_int(rng, 1, 8192)
+        n = _log_int(rng, 1, 8192 if nkv <= 8 else 3000)
         return dict(kind=kind, model=model, tokens=n, rot=rng.choice([16, 32, d // 2, d // 4 * 3, d, d]), layout=rng.choice(["half", "interleaved"]),
                     max_pos=_log_int(rng, 1024, 32768), pad=min(n // 3, rng.randint(0, 3)), keys=n > 64)
     if kind == "evict":
