@@ -55,8 +55,8 @@ def _log_int(rng, lo, hi):
 
 
 def draw(rng):
-    """One more case: tables of 64 to 131072 positions, 1 to 8192 rotated tokens (to 3000 of 32 and more kv heads), prefixes of 0 to 8192 and own caches of 0 to 4096 tokens in
-    1 to 64 sequences, evictions from caches of 1 to 12000 tokens."""
+    """One more case: tables of 64 to 131072 positions, 1 to 8192 rotated tokens (to 3000 of 32 and more kv heads), prefixes of 0 to 8192 (4096)
+    and own caches of 0 to 4096 tokens in 1 to 64 sequences, evictions from caches of 1 to 12000 tokens."""
     kind = rng.choices(["tables", "rope", "shared", "weights", "evict"], [1, 2, 4, 3, 3])[0]
     model = rng.choice(list(HEADS))
     nh, nkv, d = HEADS[model]
@@ -72,13 +72,13 @@ def draw(rng):
                     max_pos=_log_int(rng, 1024, 32768), pad=min(n // 3, rng.randint(0, 3)), keys=n > 64)
     if kind == "evict":
         n = _log_int(rng, 1, 64)
-        hi = _log_int(rng, 16, min(12000, (200000 if nkv == 8 else 40000) // n))
+        hi = _log_int(rng, 16, min(12000, (100000 if nkv <= 8 else 20000) // n))
         keep = rng.randint(1, max(1, int(hi * 1.1)))
         recent = rng.randint(0, keep // 2)
         return dict(kind=kind, model=model, seqs=n, lo=rng.randint(hi // 4, hi), hi=hi, keep=keep, sinks=rng.randint(0, min(8, keep - recent)), recent=recent)
     n = _log_int(rng, 1, 64 if kind == "shared" else 24)
-    prefix = _log_int(rng, 16, 8192) if kind == "shared" or rng.random() < 0.5 else 0
-    hi = _log_int(rng, 1 if prefix else 16, min(4096, (60000 if nkv == 8 else 15000) // n))
+    prefix = _log_int(rng, 16, 8192 if nkv <= 8 else 4096) if kind == "shared" or rng.random() < 0.5 else 0
+    hi = _log_int(rng, 1 if prefix else 16, min(4096, (45000 if nkv <= 8 else 6000) // n))
     return dict(kind=kind, model=model, seqs=n, prefix=prefix, lo=rng.randint(0 if prefix else 1, hi), hi=hi)
 
 
