@@ -139,6 +139,132 @@ hs_status hs_k_attn_decode_noalloc(const void* q, int64_t ldq, const void* pool,
                                    int32_t head_dim, int32_t max_blocks, int32_t max_ctx,
                                    void* stream);
 
+/* ---- Operators of caches beyond one sequence's plain decode step ----
+ *
+ * Rotation tables for long contexts, rotation and cache append where position
+ * and slot differ, decode attention for sequences that share a prefix, decode
+ * attention that also accumulates the weight of every cached token, and
+ * eviction by that weight. A step of a batch under a cache budget is
+ * hs_k_rope_kv, hs_k_attn_decode_weights, then hs_k_kv_evict.
+ *
+ * Common to them: head_dim is 64 or 128 and n_heads / n_kv_heads 1 to 16. Pools are
+ * as in hs_k_attn_decode; pool_blocks is the number of blocks of the pool, and
+ * an entry of a block table or a slot outside of it is never followed. bf16
+ * matrices and the pool are 16-byte aligned, their row strides multiples of 8
+ * elements, int32 and float32 arrays 4-byte aligned. The calls allocate
+ * nothing, keep no state and may be captured into a graph; what they need is
+ * in `ws`, device memory of the caller, 16-byte aligned, of at least the bytes
+ * that the matching _ws function gives (HS_ERANGE below it). ws need not be
+ * cleared, and calls that may overlap in time need one each, replays of
+ * captured calls too. Buffers and the stream belong to the current device.
+ * Results are deterministic. */
+
+/* How the angles of rotary positions are scaled. w_i = base^(-2 i / rot_dim) is
+ * the unscaled angle per position of pair i, t_i = original_ctx w_i / 2 pi its
+ * turns over the context that the model was trained on. */
+enum {
+  HS_ROPE_PLAIN = 0,  /* w_i */
+  HS_ROPE_LINEAR = 1, /* w_i / factor */
+  HS_ROPE_NTK = 2,    /* of base * factor^(rot_dim / (rot_dim - 2)) */
+  HS_ROPE_BANDS = 3,  /* s w_i + (1 - s) w_i / factor, s = (t_i - low) / (high - low) cut to [0, 1] */
+  HS_ROPE_YARN = 4    /* the same with 1 - s = (i - a) / max(b - a, 0.001) cut to [0, 1],
+                       * a = max(0, floor d(high)), b = min(rot_dim - 1, ceil d(low)),
+                       * d(x) = rot_dim ln(original_ctx / (2 pi x)) / (2 ln base) */
+};
+typedef struct {
+  int32_t kind;         /* HS_ROPE_* */
+  int32_t original_ctx; /* BANDS and YARN: >= 1 */
+  double factor;        /* all but PLAIN: > 0 */
+  double low, high;     /* BANDS and YARN: 0 < low < high */
+  double magnitude;     /* cos and sin are multiplied by it (> 0) */
+} hs_rope_scaling;
+
+/* cos_t[p][i] = magnitude cos(p w_i'), sin_t[p][i] = magnitude sin(p w_i') for p <
+ * max_pos, i < rot_dim / 2: device float32 [max_pos][rot_dim / 2], 16-byte
+ * aligned. rot_dim: 8 to 128, a multiple of 8; base > 1; scaling: host, NULL = plain
+ * with magnitude 1. Angles are formed in float64, so far positions are as exact as
+ * near ones. */
+hs_status hs_k_rope_tables(float* cos_t, float* sin_t, int32_t max_pos, int32_t rot_dim,
+                           double base, const hs_rope_scaling* scaling, void* stream);
+
+/* Rotation of the first rot_dim elements of every query and key head of T tokens
+ * (the rest passes as it is), and append of the rotated keys and the values to
+ * the paged cache. qkv: bf16 [T][ldqkv] (query heads, key heads, value heads);
+ * pos: device int32 [T]; slot: device int32 [T], block * 16 + offset. A token whose
+ * pos is outside [0, max_pos) is an empty row of a padded batch: nothing of it is
+ * written. One whose slot is outside the pool is rotated but not appended. Two
+ * tokens of a call have different slots. cos_t, sin_t: float32 [max_pos][rot_dim / 2],
+ * 16-byte aligned; rot_dim: 16 to head_dim, a multiple of 16. layout 0: pairs
+ * (i, i + rot_dim / 2); 1: interleaved, (2 i, 2 i + 1). q_out: bf16 [T][ldq]; k_out:
+ * bf16 [T][ldk] rotated keys, or NULL. q_out may be qkv itself, and k_out its key
+ * columns, with ldq and ldk equal to ldqkv. Float32 arithmetic, one rounding. */
+hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t* pos, const int32_t* slot,
+                       const float* cos_t, const float* sin_t, int32_t max_pos, int32_t rot_dim,
+                       int32_t layout, void* q_out, int64_t ldq, void* k_out, int64_t ldk,
+                       void* pool, int32_t pool_blocks, int32_t T, int32_t n_heads,
+                       int32_t n_kv_heads, int32_t head_dim, void* stream);
+
+/* hs_k_attn_decode for B sequences that share the first prefix_len tokens: the
+ * query of each attends over the prefix and then its own ctx[b] cached tokens.
+ * prefix: device int32 [ceil(prefix_len / 16)], the prefix's blocks (its last one
+ * may be filled in part); block_table, ctx: of each sequence's own tokens, 0 <= ctx
+ * <= max_ctx (values outside are cut to it). prefix_len and max_ctx may be 0; with
+ * max_ctx 0 block_table may be NULL, with prefix_len 0 prefix may. Tokens of a
+ * block outside the pool count as not cached; a sequence without any token gives
+ * zeros. hs_k_attn_decode_shared_ws: the workspace. */
+hs_status hs_k_attn_decode_shared_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t prefix_len, int32_t max_ctx,
+                                     uint64_t* bytes);
+hs_status hs_k_attn_decode_shared(const void* q, int64_t ldq, const void* pool,
+                                  int32_t pool_blocks, const int32_t* prefix, int32_t prefix_len,
+                                  const int32_t* block_table, const int32_t* ctx, void* out,
+                                  int64_t ldo, int32_t B, int32_t n_heads, int32_t n_kv_heads,
+                                  int32_t head_dim, int32_t max_blocks, int32_t max_ctx, void* ws,
+                                  uint64_t ws_bytes, void* stream);
+
+/* The same attention, and the weight that each own token received: with p[h][t]
+ * the probability that query head h gave to token t of sequence b,
+ *   acc_out[b][k][t] = decay acc[b][k][t] + sum over the query heads h of kv head k of p[h][t]
+ * for t < ctx[b] - 1; the newest token, t = ctx[b] - 1, starts at its sum (acc is not
+ * read there), and pos[b][k][ctx[b] - 1] = seen[b] - 1, the position of the newest of
+ * the seen[b] tokens of the sequence. acc, acc_out: device float32
+ * [B][n_kv_heads][acc_stride], acc_stride >= max_ctx; pos: int32 of the same shape, or
+ * NULL (seen is then not read); seen: device int32 [B]. acc_out may be acc. What
+ * lies at or past ctx[b] is left as it was. decay >= 0, finite. */
+hs_status hs_k_attn_decode_weights_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads,
+                                      int32_t head_dim, int32_t prefix_len, int32_t max_ctx,
+                                      uint64_t* bytes);
+hs_status hs_k_attn_decode_weights(const void* q, int64_t ldq, const void* pool,
+                                   int32_t pool_blocks, const int32_t* prefix, int32_t prefix_len,
+                                   const int32_t* block_table, const int32_t* ctx, void* out,
+                                   int64_t ldo, const float* acc, float* acc_out,
+                                   int64_t acc_stride, float decay, int32_t* pos,
+                                   const int32_t* seen, int32_t B, int32_t n_heads,
+                                   int32_t n_kv_heads, int32_t head_dim, int32_t max_blocks,
+                                   int32_t max_ctx, void* ws, uint64_t ws_bytes, void* stream);
+
+/* Eviction: of each kv head of each sequence with more than `keep` cached tokens
+ * the `keep` best stay: those with pos < sinks or pos >= seen[b] - recent first, then by
+ * acc, largest first (a NaN last), then the lower slot (protected ones among
+ * themselves by slot alone). The tokens that stay are packed into slots [0, keep):
+ * one whose slot is below keep does not move; the j-th slot below keep that became
+ * free takes the j-th token that stays at or past keep: its key and value in the
+ * pool, its acc and pos. acc, pos: device [B][n_kv_heads][stride]; acc_out, pos_out:
+ * [B][n_kv_heads][out_stride], entries t < ctx_out[b] are written (rows of at most keep
+ * tokens are copied); they may be acc and pos themselves, with the same stride.
+ * ctx_out[b] = min(ctx[b], keep), and may not be ctx. The sequences' own blocks are
+ * distinct. stride >= max_ctx, out_stride >= min(keep, max_ctx); keep >= 1, sinks and
+ * recent >= 0. A move from or to a block outside the pool is left out. */
+hs_status hs_k_kv_evict_ws(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx,
+                           uint64_t* bytes);
+hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_t* block_table,
+                        const int32_t* ctx, const int32_t* seen, const float* acc,
+                        const int32_t* pos, int64_t stride, float* acc_out, int32_t* pos_out,
+                        int64_t out_stride, int32_t* ctx_out, int32_t keep, int32_t sinks,
+                        int32_t recent, int32_t B, int32_t n_kv_heads, int32_t head_dim,
+                        int32_t max_blocks, int32_t max_ctx, void* ws, uint64_t ws_bytes,
+                        void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,289 @@
+// Entry points of the cache operators (include/hs_kernel.h): argument checks,
+// workspace sizes and the launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <string>
+
+#include "../../include/hs_kernel.h"
+#include "hs_host.h"
+#include "hs_kernels.h"
+
+using namespace hs;
+
+namespace {
+hs_status done(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidValue) return fail(HS_EINVAL, std::string(what) + ": unsupported shape");
+  if (e != hipSuccess) return fail(HS_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+  return HS_OK;
+}
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// HS_OK, or HS_EINVAL with the message set.
+hs_status heads_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(HS_EINVAL, "head_dim must be 64 or 128");
+  if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || n_heads / n_kv_heads > 16 ||
+      n_heads > 65536)
+    return fail(HS_EINVAL, "bad head counts");
+  return HS_OK;
+}
+
+hs_status ws_ok(const void* ws, uint64_t bytes, uint64_t need) {
+  if (bytes < need)
+    return fail(HS_ERANGE, "workspace of " + std::to_string(bytes) + " bytes, needs " + std::to_string(need));
+  if (need && !ws) return fail(HS_EINVAL, "null workspace");
+  if (!aligned(ws, 16)) return fail(HS_EINVAL, "workspace not 16-byte aligned");
+  return HS_OK;
+}
+
+// Angle per position of every pair, in turns.
+hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, double* turns) {
+  constexpr double kTwoPi = 6.283185307179586476925;
+  if (c.kind < HS_ROPE_PLAIN || c.kind > HS_ROPE_YARN) return fail(HS_EINVAL, "unknown rotary scaling");
+  if (!(c.magnitude > 0) || !std::isfinite(c.magnitude)) return fail(HS_EINVAL, "magnitude must be positive");
+  const bool banded = c.kind == HS_ROPE_BANDS || c.kind == HS_ROPE_YARN;
+  if (c.kind != HS_ROPE_PLAIN && (!(c.factor > 0) || !std::isfinite(c.factor)))
+    return fail(HS_EINVAL, "factor must be positive");
+  if (banded && (c.original_ctx < 1 || !(c.low > 0) || !(c.low < c.high) || !std::isfinite(c.high)))
+    return fail(HS_EINVAL, "needs original_ctx >= 1 and 0 < low < high");
+  if (c.kind == HS_ROPE_NTK) base *= pow(c.factor, rot / (rot - 2.0));
+  if (!(base > 1) || !std::isfinite(base)) return fail(HS_EINVAL, "base must be above 1");
+  const auto at = [&](double x) { return rot * log(c.original_ctx / (kTwoPi * x)) / (2 * log(base)); };
+  const double a = banded ? std::max(0.0, floor(at(c.high))) : 0.0;
+  const double b = banded ? std::min(rot - 1.0, ceil(at(c.low))) : 0.0;
+  for (int i = 0; i < rot / 2; ++i) {
+    double w = pow(base, -2.0 * i / rot), keep = 1.0;  // the share of w that is not stretched
+    if (c.kind == HS_ROPE_LINEAR) keep = 0.0;
+    if (c.kind == HS_ROPE_BANDS) keep = (c.original_ctx * w / kTwoPi - c.low) / (c.high - c.low);
+    if (c.kind == HS_ROPE_YARN) keep = 1.0 - (i - a) / std::max(b - a, 1e-3);
+    keep = std::min(1.0, std::max(0.0, keep));
+    if (keep < 1.0) w = (1.0 - keep) * w / c.factor + keep * w;
+    turns[i] = w / kTwoPi;
+  }
+  return HS_OK;
+}
+}  // namespace
+
+extern "C" hs_status hs_k_rope_tables(float* cos_t, float* sin_t, int32_t max_pos, int32_t rot_dim,
+                                      double base, const hs_rope_scaling* scaling, void* stream) {
+  try {
+    if (!cos_t || !sin_t || max_pos < 1) return fail(HS_EINVAL, "bad arguments");
+    if (rot_dim < 8 || rot_dim > 128 || rot_dim % 8)
+      return fail(HS_EINVAL, "rot_dim must be a multiple of 8 up to 128");
+    if (!aligned(cos_t, 16) || !aligned(sin_t, 16)) return fail(HS_EINVAL, "tables not 16-byte aligned");
+    const hs_rope_scaling plain{HS_ROPE_PLAIN, 0, 1.0, 0.0, 0.0, 1.0};
+    const hs_rope_scaling& c = scaling ? *scaling : plain;
+    double turns[64];
+    const hs_status r = rope_turns(rot_dim, base, c, turns);
+    if (r != HS_OK) return r;
+    return done(rope_tables(cos_t, sin_t, max_pos, rot_dim / 2, turns, (float)c.magnitude,
+                            static_cast<hipStream_t>(stream)),
+                "rope_tables");
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+extern "C" hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t* pos,
+                                  const int32_t* slot, const float* cos_t, const float* sin_t,
+                                  int32_t max_pos, int32_t rot_dim, int32_t layout, void* q_out,
+                                  int64_t ldq, void* k_out, int64_t ldk, void* pool,
+                                  int32_t pool_blocks, int32_t T, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t head_dim, void* stream) {
+  try {
+    if (!qkv || !pos || !slot || !cos_t || !sin_t || !q_out || !pool || T < 1 || max_pos < 1 ||
+        pool_blocks < 1)
+      return fail(HS_EINVAL, "bad arguments");
+    const hs_status h = heads_ok(n_heads, n_kv_heads, head_dim);
+    if (h != HS_OK) return h;
+    if (rot_dim < 16 || rot_dim > head_dim || rot_dim % 16)
+      return fail(HS_EINVAL, "rot_dim must be a multiple of 16 up to head_dim");
+    if (layout != 0 && layout != 1) return fail(HS_EINVAL, "layout must be 0 or 1");
+    if (ldqkv < (int64_t)(n_heads + 2 * n_kv_heads) * head_dim || ldq < (int64_t)n_heads * head_dim ||
+        (k_out && ldk < (int64_t)n_kv_heads * head_dim))
+      return fail(HS_EINVAL, "rows narrower than their heads");
+    if (ldqkv % 8 || ldq % 8 || (k_out && ldk % 8) || !aligned(qkv, 16) || !aligned(q_out, 16) ||
+        !aligned(k_out, 16) || !aligned(pool, 16) || !aligned(cos_t, 16) || !aligned(sin_t, 16) ||
+        !aligned(pos, 4) || !aligned(slot, 4))
+      return fail(HS_EINVAL, "pointers or row strides not aligned");
+    RopeKvAtArgs a{static_cast<const bf16_t*>(qkv), ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim,
+                   layout == 1, static_cast<bf16_t*>(q_out), ldq, static_cast<bf16_t*>(k_out), k_out ? ldk : 0,
+                   static_cast<bf16_t*>(pool), pool_blocks, T, n_heads, n_kv_heads, head_dim};
+    return done(rope_kv_at(a, static_cast<hipStream_t>(stream)), "rope_kv");
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+namespace {
+hs_status cache_attn_sizes(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           int32_t prefix_len, int32_t max_ctx) {
+  if (B < 1 || B > 65535 || prefix_len < 0 || max_ctx < 0 || prefix_len > 0x7FFFFFF0 || max_ctx > 0x7FFFFFF0)
+    return fail(HS_EINVAL, "bad arguments");
+  return heads_ok(n_heads, n_kv_heads, head_dim);
+}
+
+hs_status cache_attn_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                        int32_t prefix_len, int32_t max_ctx, bool weights, uint64_t* bytes) {
+  if (!bytes) return fail(HS_EINVAL, "bad arguments");
+  const hs_status r = cache_attn_sizes(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx);
+  if (r != HS_OK) return r;
+  *bytes = 4ull * cache_attn_plan(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx, weights).floats;
+  return HS_OK;
+}
+
+hs_status cache_attn_call(CacheAttnArgs a, bool weights, void* ws, uint64_t ws_bytes, void* stream) {
+  const hs_status r = cache_attn_sizes(a.B, a.n_heads, a.n_kv_heads, a.D, a.prefix_len, a.max_ctx);
+  if (r != HS_OK) return r;
+  if (!a.q || !a.pool || !a.ctx || !a.out || a.pool_blocks < 1 || (a.prefix_len && !a.prefix) ||
+      (a.max_ctx && !a.block_table))
+    return fail(HS_EINVAL, "bad arguments");
+  a.G = a.n_heads / a.n_kv_heads;
+  if (a.max_ctx && a.max_blocks < (a.max_ctx + 15) / 16) return fail(HS_EINVAL, "block table too narrow");
+  if (a.ldq < (int64_t)a.n_heads * a.D || a.ldo < (int64_t)a.n_heads * a.D)
+    return fail(HS_EINVAL, "rows narrower than their heads");
+  if (a.ldq % 8 || !aligned(a.q, 16) || !aligned(a.pool, 16) || !aligned(a.out, 4) || a.ldo % 2 ||
+      !aligned(a.prefix, 4) || !aligned(a.block_table, 4) || !aligned(a.ctx, 4))
+    return fail(HS_EINVAL, "pointers or row strides not aligned");
+  if (weights) {
+    if (a.max_ctx && (!a.acc || !a.acc_out)) return fail(HS_EINVAL, "null weights");
+    if (a.acc_stride < a.max_ctx) return fail(HS_EINVAL, "rows of weights shorter than max_ctx");
+    if (!(a.decay >= 0) || !std::isfinite(a.decay)) return fail(HS_EINVAL, "decay must be finite and not negative");
+    if (a.pos && !a.seen) return fail(HS_EINVAL, "positions without the tokens seen");
+    if (!aligned(a.acc, 4) || !aligned(a.acc_out, 4) || !aligned(a.pos, 4) || !aligned(a.seen, 4))
+      return fail(HS_EINVAL, "pointers or row strides not aligned");
+  }
+  const CacheAttnPlan p =
+      cache_attn_plan(a.B, a.n_heads, a.n_kv_heads, a.D, a.prefix_len, a.max_ctx, weights);
+  const hs_status w = ws_ok(ws, ws_bytes, 4ull * p.floats);
+  if (w != HS_OK) return w;
+  return done(cache_attn(a, p, static_cast<float*>(ws), static_cast<hipStream_t>(stream)), "cache attention");
+}
+}  // namespace
+
+extern "C" hs_status hs_k_attn_decode_shared_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads,
+                                                int32_t head_dim, int32_t prefix_len,
+                                                int32_t max_ctx, uint64_t* bytes) {
+  try {
+    return cache_attn_ws(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx, false, bytes);
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+extern "C" hs_status hs_k_attn_decode_shared(
+    const void* q, int64_t ldq, const void* pool, int32_t pool_blocks, const int32_t* prefix,
+    int32_t prefix_len, const int32_t* block_table, const int32_t* ctx, void* out, int64_t ldo,
+    int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_blocks,
+    int32_t max_ctx, void* ws, uint64_t ws_bytes, void* stream) {
+  try {
+    CacheAttnArgs a{};
+    a.q = static_cast<const bf16_t*>(q), a.ldq = ldq;
+    a.pool = static_cast<const bf16_t*>(pool), a.pool_blocks = pool_blocks;
+    a.prefix = prefix, a.prefix_len = prefix_len;
+    a.block_table = block_table, a.ctx = ctx;
+    a.out = static_cast<bf16_t*>(out), a.ldo = ldo;
+    a.B = B, a.n_heads = n_heads, a.n_kv_heads = n_kv_heads, a.D = head_dim;
+    a.max_blocks = max_blocks, a.max_ctx = max_ctx;
+    return cache_attn_call(a, false, ws, ws_bytes, stream);
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+extern "C" hs_status hs_k_attn_decode_weights_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads,
+                                                 int32_t head_dim, int32_t prefix_len,
+                                                 int32_t max_ctx, uint64_t* bytes) {
+  try {
+    return cache_attn_ws(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx, true, bytes);
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+extern "C" hs_status hs_k_attn_decode_weights(
+    const void* q, int64_t ldq, const void* pool, int32_t pool_blocks, const int32_t* prefix,
+    int32_t prefix_len, const int32_t* block_table, const int32_t* ctx, void* out, int64_t ldo,
+    const float* acc, float* acc_out, int64_t acc_stride, float decay, int32_t* pos,
+    const int32_t* seen, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+    int32_t max_blocks, int32_t max_ctx, void* ws, uint64_t ws_bytes, void* stream) {
+  try {
+    CacheAttnArgs a{};
+    a.q = static_cast<const bf16_t*>(q), a.ldq = ldq;
+    a.pool = static_cast<const bf16_t*>(pool), a.pool_blocks = pool_blocks;
+    a.prefix = prefix, a.prefix_len = prefix_len;
+    a.block_table = block_table, a.ctx = ctx;
+    a.out = static_cast<bf16_t*>(out), a.ldo = ldo;
+    a.acc = acc, a.acc_out = acc_out, a.acc_stride = acc_stride, a.decay = decay;
+    a.pos = pos, a.seen = seen;
+    a.B = B, a.n_heads = n_heads, a.n_kv_heads = n_kv_heads, a.D = head_dim;
+    a.max_blocks = max_blocks, a.max_ctx = max_ctx;
+    return cache_attn_call(a, true, ws, ws_bytes, stream);
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+namespace {
+hs_status evict_sizes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
+  if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || keep < 1 || max_ctx < 1 || max_ctx > 0x7FFFFFF0)
+    return fail(HS_EINVAL, "bad arguments");
+  return HS_OK;
+}
+// moves a row can have
+int64_t evict_cap(int32_t keep, int32_t max_ctx) {
+  return std::max<int64_t>(0, std::min<int64_t>(keep, (int64_t)max_ctx - keep));
+}
+uint64_t evict_bytes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
+  return 8ull * B * n_kv_heads * evict_cap(keep, max_ctx);
+}
+}  // namespace
+
+extern "C" hs_status hs_k_kv_evict_ws(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx,
+                                      uint64_t* bytes) {
+  try {
+    if (!bytes) return fail(HS_EINVAL, "bad arguments");
+    const hs_status r = evict_sizes(B, n_kv_heads, keep, max_ctx);
+    if (r != HS_OK) return r;
+    *bytes = evict_bytes(B, n_kv_heads, keep, max_ctx);
+    return HS_OK;
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}
+
+extern "C" hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_t* block_table,
+                                   const int32_t* ctx, const int32_t* seen, const float* acc,
+                                   const int32_t* pos, int64_t stride, float* acc_out,
+                                   int32_t* pos_out, int64_t out_stride, int32_t* ctx_out,
+                                   int32_t keep, int32_t sinks, int32_t recent, int32_t B,
+                                   int32_t n_kv_heads, int32_t head_dim, int32_t max_blocks,
+                                   int32_t max_ctx, void* ws, uint64_t ws_bytes, void* stream) {
+  try {
+    const hs_status r = evict_sizes(B, n_kv_heads, keep, max_ctx);
+    if (r != HS_OK) return r;
+    if (!pool || !block_table || !ctx || !seen || !acc || !pos || !acc_out || !pos_out || !ctx_out ||
+        pool_blocks < 1 || sinks < 0 || recent < 0 || ctx_out == ctx)
+      return fail(HS_EINVAL, "bad arguments");
+    if (head_dim != 64 && head_dim != 128) return fail(HS_EINVAL, "head_dim must be 64 or 128");
+    if (max_blocks < (max_ctx + 15) / 16) return fail(HS_EINVAL, "block table too narrow");
+    if (stride < max_ctx || out_stride < std::min(keep, max_ctx))
+      return fail(HS_EINVAL, "rows of weights shorter than their tokens");
+    if ((static_cast<const void*>(acc) == acc_out || static_cast<const void*>(pos) == pos_out) && stride != out_stride)
+      return fail(HS_EINVAL, "weights written in place need one stride");
+    if (!aligned(pool, 16) || !aligned(block_table, 4) || !aligned(ctx, 4) || !aligned(seen, 4) ||
+        !aligned(acc, 4) || !aligned(pos, 4) || !aligned(acc_out, 4) || !aligned(pos_out, 4) ||
+        !aligned(ctx_out, 4))
+      return fail(HS_EINVAL, "pointers not aligned");
+    const hs_status w = ws_ok(ws, ws_bytes, evict_bytes(B, n_kv_heads, keep, max_ctx));
+    if (w != HS_OK) return w;
+    KvEvictArgs a{static_cast<bf16_t*>(pool), pool_blocks, block_table, ctx, seen, acc, pos, stride,
+                  acc_out, pos_out, out_stride, ctx_out, keep, sinks, recent, B, n_kv_heads, head_dim,
+                  max_blocks, max_ctx, static_cast<int32_t*>(ws), (int)evict_cap(keep, max_ctx)};
+    return done(kv_evict(a, static_cast<hipStream_t>(stream)), "kv_evict");
+  } catch (...) {
+    return fail(HS_EINVAL, "unexpected internal error");
+  }
+}

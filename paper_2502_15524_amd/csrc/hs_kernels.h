@@ -152,4 +152,65 @@ hipError_t meta_pull(const int32_t* host, int32_t* dev, int64_t n, hipStream_t s
 hipError_t kv_copy(const uint64_t* src, const uint64_t* dst, const int32_t* valid, int n_units,
                    int64_t unit_bytes, int D, int zero_tail, hipStream_t s, LaunchInfo* info);
 
+// cos and sin of 2 pi p turns[i], times magnitude: [max_pos][half] each.
+hipError_t rope_tables(float* cos_t, float* sin_t, int max_pos, int half, const double* turns,
+                       float magnitude, hipStream_t s);
+
+// Rotation of the first `rot` elements of every query and key head at given
+// positions, and cache append at given slots.
+struct RopeKvAtArgs {
+  const bf16_t* qkv; int64_t ldqkv;        // [T][ldqkv]: q heads, k heads, v heads
+  const int32_t* pos;                      // [T] position; outside [0, max_pos): an empty row
+  const int32_t* slot;                     // [T] block * 16 + offset; outside the pool: no append
+  const float* cos_t; const float* sin_t;  // [max_pos][rot / 2]
+  int max_pos, rot;
+  bool interleaved;
+  bf16_t* q_out; int64_t ldq;
+  bf16_t* k_out; int64_t ldk;              // or null
+  bf16_t* pool; int pool_blocks;
+  int T, n_heads, n_kv_heads, D;
+};
+hipError_t rope_kv_at(const RopeKvAtArgs& a, hipStream_t s);
+
+// Decode attention over a shared prefix and each sequence's own cache, and the
+// weights of the own tokens (acc_out set).
+struct CacheAttnArgs {
+  const bf16_t* q; int64_t ldq;
+  const bf16_t* pool; int pool_blocks;
+  const int32_t* prefix; int prefix_len;   // blocks of the prefix, its tokens
+  const int32_t* block_table;              // [B][max_blocks]
+  const int32_t* ctx;                      // [B] own tokens
+  bf16_t* out; int64_t ldo;
+  const float* acc; float* acc_out; int64_t acc_stride;  // [B][n_kv_heads][acc_stride]
+  float decay;
+  int32_t* pos; const int32_t* seen;       // positions (may be null), tokens seen [B]
+  int B, n_heads, n_kv_heads, G, D, max_blocks, max_ctx;
+  // set by cache_attn from its plan
+  int lead_blocks, splits;
+  float *part_o, *part_ml, *scores;
+  int64_t score_stride;
+};
+// How a call is cut, and its workspace (offsets in floats).
+struct CacheAttnPlan {
+  int lead_blocks;                         // prefix blocks before a sequence's own
+  int64_t splits, score_stride;
+  int64_t part_o, part_ml, scores, floats;
+};
+CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t D,
+                              int64_t prefix_len, int64_t max_ctx, bool weights);
+hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStream_t s);
+
+struct KvEvictArgs {
+  bf16_t* pool; int pool_blocks;
+  const int32_t* block_table;              // [B][max_blocks]
+  const int32_t* ctx; const int32_t* seen; // [B]
+  const float* acc; const int32_t* pos; int64_t stride;  // [B][n_kv_heads][stride]
+  float* acc_out; int32_t* pos_out; int64_t out_stride;
+  int32_t* ctx_out;                        // [B]
+  int keep, sinks, recent;
+  int B, n_kv_heads, D, max_blocks, max_ctx;
+  int32_t* lists; int cap;                 // [B][n_kv_heads][2][cap] holes and what fills them
+};
+hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s);
+
 }  // namespace hs

@@ -10,6 +10,7 @@ built, every call raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "libhs.so")
@@ -73,6 +74,11 @@ class hs_kernel_stat(C.Structure):
                 ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class hs_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("original_ctx", C.c_int32), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
+
+
 _P = C.c_void_p
 _SIGS = {
     "hs_weight_layout": [C.POINTER(hs_model_cfg), C.c_int32, C.c_int32,
@@ -129,6 +135,21 @@ _SIGS = {
     "hs_k_attn_decode_rope": [_P, C.c_int64, _P, _P, _P, _P, _P, C.c_int32, _P, C.c_int64,
                               C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                               _P],
+    "hs_k_rope_tables": [_P, _P, C.c_int32, C.c_int32, C.c_double, C.POINTER(hs_rope_scaling),
+                         _P],
+    "hs_k_rope_kv": [_P, C.c_int64, _P, _P, _P, _P, C.c_int32, C.c_int32, C.c_int32, _P,
+                     C.c_int64, _P, C.c_int64, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                     C.c_int32, _P],
+    "hs_k_attn_decode_shared_ws": [C.c_int32] * 6 + [C.POINTER(C.c_uint64)],
+    "hs_k_attn_decode_shared": [_P, C.c_int64, _P, C.c_int32, _P, C.c_int32, _P, _P, _P,
+                                C.c_int64] + [C.c_int32] * 6 + [_P, C.c_uint64, _P],
+    "hs_k_attn_decode_weights_ws": [C.c_int32] * 6 + [C.POINTER(C.c_uint64)],
+    "hs_k_attn_decode_weights": [_P, C.c_int64, _P, C.c_int32, _P, C.c_int32, _P, _P, _P,
+                                 C.c_int64, _P, _P, C.c_int64, C.c_float, _P, _P]
+                                + [C.c_int32] * 6 + [_P, C.c_uint64, _P],
+    "hs_k_kv_evict_ws": [C.c_int32] * 4 + [C.POINTER(C.c_uint64)],
+    "hs_k_kv_evict": [_P, C.c_int32, _P, _P, _P, _P, _P, C.c_int64, _P, _P, C.c_int64, _P]
+                     + [C.c_int32] * 8 + [_P, C.c_uint64, _P],
 }
 EXPORTED = sorted(list(_SIGS) + ["hs_last_error"])
 
@@ -454,3 +475,94 @@ def hs_k_attn_decode_rope(qkv, ldqkv, pool, block_table, ctx, cos_t, sin_t, max_
 
 def hs_k_rmsnorm(x, g, out, rows, hidden, eps, stream=0):
     _check(lib().hs_k_rmsnorm(x, g, out, rows, hidden, eps, stream or None))
+
+
+ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+
+
+def rope_scaling(kind="plain", factor=1.0, original_ctx=0, low=1.0, high=None, magnitude=None):
+    """A scaling of rotary angles for hs_k_rope_tables. high: 4 turns for "bands", 32 for
+    "yarn"; magnitude: 0.1 ln(factor) + 1 for "yarn" (factor above 1), else 1."""
+    if isinstance(kind, str):
+        kind = ROPE_SCALING[kind]
+    yarn = kind == ROPE_SCALING["yarn"]
+    if high is None:
+        high = 32.0 if yarn else 4.0
+    if magnitude is None:
+        magnitude = 0.1 * math.log(factor) + 1.0 if yarn and factor > 1 else 1.0
+    return hs_rope_scaling(kind, original_ctx, factor, low, high, magnitude)
+
+
+def hs_k_rope_tables(cos_t, sin_t, max_pos, rot_dim, base, scaling=None, stream=0):
+    """cos and sin tables [max_pos][rot_dim / 2] of (scaled) rotary positions."""
+    _check(lib().hs_k_rope_tables(cos_t, sin_t, max_pos, rot_dim, base,
+                                  None if scaling is None else C.byref(scaling), stream or None))
+
+
+def hs_k_rope_kv(qkv, ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim, layout, q_out, ldq, k_out,
+                 ldk, pool, pool_blocks, T, n_heads, n_kv_heads, head_dim, stream=0):
+    """Rotation at given positions and append to the paged cache at given slots; layout:
+    "half" or "interleaved"; k_out 0: no rows of rotated keys."""
+    if isinstance(layout, str):
+        layout = ROPE_LAYOUT[layout]
+    _check(lib().hs_k_rope_kv(qkv, ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim, layout, q_out,
+                              ldq, k_out or None, ldk, pool, pool_blocks, T, n_heads, n_kv_heads,
+                              head_dim, stream or None))
+
+
+def _bytes_of(fn, *args):
+    n = C.c_uint64(0)
+    _check(fn(*args, C.byref(n)))
+    return n.value
+
+
+def hs_k_attn_decode_shared_ws(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
+    """Bytes of workspace of hs_k_attn_decode_shared."""
+    return _bytes_of(lib().hs_k_attn_decode_shared_ws, B, n_heads, n_kv_heads, head_dim,
+                     prefix_len, max_ctx)
+
+
+def hs_k_attn_decode_shared(q, ldq, pool, pool_blocks, prefix, prefix_len, block_table, ctx, out,
+                            ldo, B, n_heads, n_kv_heads, head_dim, max_blocks, max_ctx, ws,
+                            ws_bytes, stream=0):
+    """Decode attention of sequences that share a prefix: the prefix's blocks, then each
+    sequence's own (ctx: own tokens, which may be 0)."""
+    _check(lib().hs_k_attn_decode_shared(q, ldq, pool, pool_blocks, prefix or None, prefix_len,
+                                         block_table or None, ctx, out, ldo, B, n_heads,
+                                         n_kv_heads, head_dim, max_blocks, max_ctx, ws, ws_bytes,
+                                         stream or None))
+
+
+def hs_k_attn_decode_weights_ws(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
+    """Bytes of workspace of hs_k_attn_decode_weights."""
+    return _bytes_of(lib().hs_k_attn_decode_weights_ws, B, n_heads, n_kv_heads, head_dim,
+                     prefix_len, max_ctx)
+
+
+def hs_k_attn_decode_weights(q, ldq, pool, pool_blocks, prefix, prefix_len, block_table, ctx, out,
+                             ldo, acc, acc_out, acc_stride, decay, pos, seen, B, n_heads,
+                             n_kv_heads, head_dim, max_blocks, max_ctx, ws, ws_bytes, stream=0):
+    """hs_k_attn_decode_shared that also accumulates, per kv head, the weight that every own
+    token received, and records the newest token's position (pos 0: not)."""
+    _check(lib().hs_k_attn_decode_weights(q, ldq, pool, pool_blocks, prefix or None, prefix_len,
+                                          block_table or None, ctx, out, ldo, acc or None,
+                                          acc_out or None, acc_stride, decay, pos or None,
+                                          seen or None, B, n_heads, n_kv_heads, head_dim,
+                                          max_blocks, max_ctx, ws, ws_bytes, stream or None))
+
+
+def hs_k_kv_evict_ws(B, n_kv_heads, keep, max_ctx):
+    """Bytes of workspace of hs_k_kv_evict."""
+    return _bytes_of(lib().hs_k_kv_evict_ws, B, n_kv_heads, keep, max_ctx)
+
+
+def hs_k_kv_evict(pool, pool_blocks, block_table, ctx, seen, acc, pos, stride, acc_out, pos_out,
+                  out_stride, ctx_out, keep, sinks, recent, B, n_kv_heads, head_dim, max_blocks,
+                  max_ctx, ws, ws_bytes, stream=0):
+    """Keeps the `keep` best tokens of every kv head of every sequence, packed into the first
+    `keep` slots."""
+    _check(lib().hs_k_kv_evict(pool, pool_blocks, block_table, ctx, seen, acc, pos, stride,
+                               acc_out, pos_out, out_stride, ctx_out, keep, sinks, recent, B,
+                               n_kv_heads, head_dim, max_blocks, max_ctx, ws, ws_bytes,
+                               stream or None))

@@ -1,0 +1,94 @@
+"""What the cache operators refuse, before anything reaches a GPU, and their workspace sizes."""
+import math
+
+import pytest
+
+from paper_2502_15524_amd import hs
+
+P = 1 << 20  # any aligned non-null value: nothing is dereferenced or launched
+
+
+def refused(code, fn, *args, **kw):
+    with pytest.raises(hs.HSError) as e:
+        fn(*args, **kw)
+    assert e.value.code == code, e.value
+
+
+@pytest.mark.parametrize("change", [
+    dict(cos_t=0), dict(sin_t=P + 4), dict(max_pos=0), dict(rot_dim=4), dict(rot_dim=136), dict(rot_dim=20), dict(base=1.0),
+    dict(base=math.nan), dict(base=math.inf), dict(scaling=hs.hs_rope_scaling(5, 100, 2.0, 1.0, 4.0, 1.0)),
+    dict(scaling=hs.rope_scaling("linear", factor=0.0)), dict(scaling=hs.rope_scaling("ntk", factor=math.inf)),
+    dict(scaling=hs.rope_scaling("bands", factor=2.0)), dict(scaling=hs.rope_scaling("bands", factor=2.0, original_ctx=10, low=4.0)),
+    dict(scaling=hs.rope_scaling("yarn", factor=2.0, original_ctx=10, low=0.0)),
+    dict(scaling=hs.rope_scaling("yarn", factor=2.0, original_ctx=10, high=math.inf)),
+    dict(scaling=hs.rope_scaling("linear", factor=2.0, magnitude=0.0)), dict(scaling=hs.rope_scaling("ntk", factor=1e300)),
+    dict(scaling=hs.rope_scaling("linear", factor=2.0, magnitude=math.nan))])
+def test_rope_tables_refuses(change):
+    a = dict(cos_t=P, sin_t=P, max_pos=64, rot_dim=64, base=10000.0, scaling=None) | change
+    refused(hs.HS_EINVAL, hs.hs_k_rope_tables, **a)
+
+
+@pytest.mark.parametrize("change", [
+    dict(qkv=0), dict(pos=0), dict(slot=0), dict(cos_t=0), dict(q_out=0), dict(pool=0), dict(T=0), dict(max_pos=0), dict(pool_blocks=0),
+    dict(rot_dim=0), dict(rot_dim=24), dict(rot_dim=144), dict(layout=2), dict(head_dim=96), dict(n_kv_heads=3), dict(n_kv_heads=0),
+    dict(n_heads=0), dict(n_heads=136), dict(ldqkv=48 * 128 - 8), dict(ldq=32 * 128 - 8), dict(k_out=P, ldk=1016), dict(ldqkv=48 * 128 + 4),
+    dict(ldq=32 * 128 + 2), dict(qkv=P + 2), dict(q_out=P + 8), dict(k_out=P + 4), dict(pool=P + 8), dict(cos_t=P + 8), dict(pos=P + 2)])
+def test_rope_kv_refuses(change):
+    a = dict(qkv=P, ldqkv=48 * 128, pos=P, slot=P, cos_t=P, sin_t=P, max_pos=64, rot_dim=128, layout="half", q_out=P, ldq=32 * 128,
+             k_out=0, ldk=1024, pool=P, pool_blocks=4, T=3, n_heads=32, n_kv_heads=8, head_dim=128) | change
+    refused(hs.HS_EINVAL, hs.hs_k_rope_kv, **a)
+
+
+ATTN = dict(q=P, ldq=4096, pool=P, pool_blocks=9, prefix=P, prefix_len=100, block_table=P, ctx=P, out=P, ldo=4096, B=2, n_heads=32,
+            n_kv_heads=8, head_dim=128, max_blocks=4, max_ctx=64, ws=P, ws_bytes=1 << 40)
+WEIGHTS = ATTN | dict(acc=P, acc_out=P, acc_stride=64, decay=1.0, pos=P, seen=P)
+BAD = [dict(q=0), dict(pool=0), dict(ctx=0), dict(out=0), dict(prefix=0), dict(block_table=0), dict(pool_blocks=0), dict(prefix_len=-1),
+       dict(max_ctx=-1), dict(B=0), dict(B=65536), dict(n_heads=30), dict(n_kv_heads=0), dict(n_heads=136, ldq=1 << 20, ldo=1 << 20),
+       dict(head_dim=80), dict(max_ctx=65), dict(max_blocks=3), dict(ldq=4088), dict(ldo=4094), dict(ldq=4100), dict(ldo=4097), dict(q=P + 2),
+       dict(pool=P + 8), dict(out=P + 2), dict(ctx=P + 1), dict(prefix=P + 2), dict(block_table=P + 2), dict(ws=P + 8), dict(ws=0)]
+
+
+@pytest.mark.parametrize("change", BAD)
+def test_attn_decode_shared_refuses(change):
+    refused(hs.HS_EINVAL, hs.hs_k_attn_decode_shared, **(ATTN | change))
+
+
+@pytest.mark.parametrize("change", BAD + [
+    dict(acc=0), dict(acc_out=0), dict(acc_stride=63), dict(decay=-0.5), dict(decay=math.nan), dict(decay=math.inf), dict(seen=0),
+    dict(acc=P + 2), dict(acc_out=P + 1), dict(pos=P + 2)])
+def test_attn_decode_weights_refuses(change):
+    refused(hs.HS_EINVAL, hs.hs_k_attn_decode_weights, **(WEIGHTS | change))
+
+
+def test_attention_workspaces():
+    """A byte less than the size given is refused, and the sizes grow with the call."""
+    for fn, size, args in ((hs.hs_k_attn_decode_shared, hs.hs_k_attn_decode_shared_ws, ATTN),
+                           (hs.hs_k_attn_decode_weights, hs.hs_k_attn_decode_weights_ws, WEIGHTS)):
+        need = size(2, 32, 8, 128, 100, 64)
+        assert need > 0
+        refused(hs.HS_ERANGE, fn, **(args | dict(ws_bytes=need - 1)))
+        assert size(64, 40, 40, 128, 100000, 100000) > 64 * 40 * 128 * 4
+        for bad in ((0, 32, 8, 128, 1, 1), (2, 32, 8, 96, 1, 1), (2, 33, 8, 128, 1, 1), (2, 32, 8, 128, -1, 1), (2, 32, 8, 128, 1, -1)):
+            refused(hs.HS_EINVAL, size, *bad)
+    assert hs.hs_k_attn_decode_weights_ws(2, 32, 8, 128, 0, 64) > hs.hs_k_attn_decode_shared_ws(2, 32, 8, 128, 0, 64)
+
+
+EVICT = dict(pool=P, pool_blocks=9, block_table=P, ctx=P, seen=P, acc=P, pos=2 * P, stride=64, acc_out=3 * P, pos_out=4 * P, out_stride=32,
+             ctx_out=5 * P, keep=32, sinks=4, recent=8, B=2, n_kv_heads=8, head_dim=128, max_blocks=4, max_ctx=64, ws=P, ws_bytes=1 << 40)
+
+
+@pytest.mark.parametrize("change", [
+    dict(pool=0), dict(pool_blocks=0), dict(block_table=0), dict(ctx=0), dict(seen=0), dict(acc=0), dict(pos=0), dict(acc_out=0),
+    dict(pos_out=0), dict(ctx_out=0), dict(ctx_out=P), dict(keep=0), dict(sinks=-1), dict(recent=-1), dict(B=0), dict(B=65536),
+    dict(n_kv_heads=0), dict(head_dim=32), dict(max_blocks=3), dict(max_ctx=0), dict(max_ctx=65), dict(stride=63), dict(out_stride=31),
+    dict(acc_out=P), dict(pos_out=2 * P), dict(pool=P + 2), dict(acc=P + 2), dict(ctx_out=P + 2), dict(ws=P + 4), dict(ws=0)])
+def test_kv_evict_refuses(change):
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict, **(EVICT | change))
+
+
+def test_evict_workspace():
+    need = hs.hs_k_kv_evict_ws(2, 8, 32, 64)
+    assert need > 0
+    refused(hs.HS_ERANGE, hs.hs_k_kv_evict, **(EVICT | dict(ws_bytes=need - 1)))
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 2, 8, 0, 64)
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 2, 8, 4, 0)

@@ -1,0 +1,704 @@
+"""The cache operators (rotary tables, rotation with append at given positions,
+decode attention over a shared prefix, accumulated attention weights, eviction)
+against plain float64 implementations, and a run of them together.
+
+Tolerances are element by element and come from the roundings a result goes
+through: half a step of bf16 is 2^-8 of the value, of float32 2^-24."""
+import numpy as np
+import pytest
+
+from tests import gpu_util as G
+from workloads import gen
+
+BF, F32 = 2.0 ** -8, 2.0 ** -24
+BLOCK = 16
+
+pytestmark = pytest.mark.gpu
+
+
+def _hs():
+    from paper_2502_15524_amd import hs
+    return hs
+
+
+def bf(rng, shape, std=1.0):
+    return gen.round_to_bf16((rng.standard_normal(shape) * std).astype(np.float32))
+
+
+def dev(a):
+    torch = G.torch()
+    a = np.ascontiguousarray(a)
+    return torch.from_numpy(a).cuda()
+
+
+def dev_bf(a):
+    torch = G.torch()  # (every value here is one of bf16, or not finite)
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(torch.bfloat16).cuda()
+
+
+def host(x):
+    torch = G.torch()
+    return G.from_dev_bf16(x) if x.dtype == torch.bfloat16 else x.cpu().numpy()
+
+
+def workspace(nbytes):
+    torch = G.torch()
+    return torch.full((max(int(nbytes), 16),), 0xFF, dtype=torch.uint8, device="cuda")  # NaN to a float
+
+
+# ------------------------------------------------------------------- tables
+
+def turns(rot, base, kind, factor, original, low, high):
+    """w_i of every pair in long double, from the definitions."""
+    ld = np.longdouble
+    i = np.arange(rot // 2, dtype=ld)
+    base, factor = ld(base), ld(factor)
+    two_pi = 2 * np.arctan2(ld(0), ld(-1))
+    if kind == "ntk":
+        base = base * factor ** (ld(rot) / (rot - 2))
+    w = base ** (-2 * i / rot)
+    if kind == "linear":
+        w = w / factor
+    if kind == "bands":
+        s = np.clip((original * w / two_pi - low) / ld(high - low), 0, 1)
+        w = (1 - s) * w / factor + s * w
+    if kind == "yarn":
+        at = lambda x: float(rot * np.log(original / (two_pi * x)) / (2 * np.log(base)))  # noqa: E731
+        a, b = max(0, np.floor(at(high))), min(rot - 1, np.ceil(at(low)))
+        r = np.clip((i - a) / max(b - a, 1e-3), 0, 1)
+        w = r * w / factor + (1 - r) * w
+    return w
+
+
+@pytest.mark.parametrize("max_pos,rot,base,kind,factor,original,extra", [
+    (1, 8, 10000.0, "plain", 1.0, 0, {}), (1024, 64, 10000.0, "plain", 1.0, 0, {}),
+    (777, 24, 10000.0, "linear", 3.5, 0, {}), (2000, 128, 500000.0, "bands", 8.0, 300, {}),
+    (131072, 128, 500000.0, "bands", 8.0, 8192, dict(low=1.0, high=4.0)),
+    (5000, 80, 10000.0, "ntk", 4.0, 0, {}), (4097, 96, 10000.0, "yarn", 16.0, 256, {}),
+    (300, 48, 10000.0, "yarn", 1.5, 16, dict(magnitude=2.5)), (100000, 16, 1e6, "yarn", 40.0, 2500, {})])
+def test_rope_tables(max_pos, rot, base, kind, factor, original, extra):
+    """|error| <= magnitude 4 x 2^-24: half a step of the reduced angle (below 1: 2^-25),
+    two of the polynomial (2^-25 each), the magnitude's and the product's (2^-24 each)
+    make 3.5, the dropped terms (2e-9) less than the rest."""
+    torch = G.torch()
+    hs = _hs()
+    sc = hs.rope_scaling(kind, factor=factor, original_ctx=original, **extra)
+    w = turns(rot, base, kind, factor, original, sc.low, sc.high)
+    out = torch.full((2, max_pos + 1, rot // 2), 7.0, dtype=torch.float32, device="cuda")
+    hs.hs_k_rope_tables(out[0].data_ptr(), out[1].data_ptr(), max_pos, rot, base,
+                        None if kind == "plain" else sc, G.stream_ptr())
+    got = host(out)
+    pos = np.unique(np.concatenate([np.arange(min(max_pos, 70)), np.arange(max_pos - min(max_pos, 70), max_pos),
+                                    np.random.default_rng(rot).integers(0, max_pos, 500)]))
+    ang = pos.astype(np.longdouble)[:, None] * w
+    assert np.abs(got[0][pos] - np.cos(ang) * sc.magnitude).max() <= 4 * F32 * sc.magnitude
+    assert np.abs(got[1][pos] - np.sin(ang) * sc.magnitude).max() <= 4 * F32 * sc.magnitude
+    assert np.all(got[:, max_pos] == 7.0)
+
+
+def test_rope_tables_default_magnitude_is_yarns():
+    hs = _hs()
+    assert hs.rope_scaling("yarn", factor=16.0, original_ctx=256).magnitude == pytest.approx(1 + 0.1 * np.log(16))
+    assert hs.rope_scaling("bands", factor=16.0, original_ctx=256).magnitude == 1.0
+
+
+# ----------------------------------------------------------------- rotation
+
+def rotate(x, cos, sin, rot, layout):
+    """x [..., d] in float64, cos and sin [..., rot / 2]."""
+    y = np.array(x, np.float64)
+    i = np.arange(rot // 2)
+    first, second = (i, i + rot // 2) if layout == "half" else (2 * i, 2 * i + 1)
+    y[..., first] = x[..., first] * cos - x[..., second] * sin
+    y[..., second] = x[..., second] * cos + x[..., first] * sin
+    return y
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("T,nh,nkv,d,rot,layout,keys,pad", [
+    (1, 4, 4, 64, 64, "half", False, 0), (1, 32, 8, 128, 128, "interleaved", True, 0),
+    (17, 32, 8, 128, 128, "half", True, 2), (131, 8, 8, 128, 96, "half", True, 3),
+    (131, 40, 40, 128, 64, "interleaved", True, 3), (64, 4, 4, 64, 16, "interleaved", False, 1),
+    (33, 6, 2, 64, 48, "half", True, 0), (19, 48, 3, 128, 16, "half", False, 5), (1000, 4, 1, 64, 32, "half", True, 0)])
+def test_rope_kv(T, nh, nkv, d, rot, layout, keys, pad, in_place):
+    """Rotated values within one bf16 rounding (and three float32 ones of the two
+    products), values and untouched elements bit for bit, nothing written outside
+    the rows and slots named. Positions and slots are unrelated; rows of padding
+    carry garbage."""
+    torch = G.torch()
+    hs = _hs()
+    rng = np.random.default_rng(T * 7 + nh + rot)
+    width, max_pos, blocks = (nh + 2 * nkv) * d, 300, -(-T // 16) + 3
+    ldqkv, ldq, ldk = width + 24, nh * d + 8, nkv * d + 16
+    qkv = bf(rng, (T, ldqkv), 1.5)
+    pos = rng.integers(0, max_pos, T).astype(np.int32)
+    pos[rng.permutation(T)[:1]] = max_pos - 1
+    slot = rng.permutation(blocks * BLOCK)[:T].astype(np.int32)
+    empty = rng.permutation(T)[:pad]
+    pos[empty] = [-1, max_pos, -2 ** 31, 2 ** 31 - 1, -7][:pad]
+    qkv[empty] = np.nan
+    uncached = rng.permutation(T)[:T // 8]
+    slot[uncached] = ([-1, blocks * BLOCK, 2 ** 31 - 1] * T)[:T // 8]
+    ang = rng.uniform(0, 6.28, (max_pos, rot // 2))
+    cos, sin = np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+    pool = bf(rng, (blocks, 2, nkv, BLOCK, d))
+    x, q_out, k_out, dpool = dev_bf(qkv), dev_bf(bf(rng, (T + 1, ldq))), dev_bf(bf(rng, (T + 1, ldk))), dev_bf(pool)
+    q0, k0 = host(q_out), host(k_out)
+    if in_place:
+        q_ptr, k_ptr, ldq, ldk = x.data_ptr(), x.data_ptr() + nh * d * 2, ldqkv, ldqkv
+    else:
+        q_ptr, k_ptr = q_out.data_ptr(), k_out.data_ptr()
+    dpos, dslot, dcos, dsin = dev(pos), dev(slot), dev(cos), dev(sin)
+    hs.hs_k_rope_kv(x.data_ptr(), ldqkv, dpos.data_ptr(), dslot.data_ptr(), dcos.data_ptr(), dsin.data_ptr(), max_pos, rot,
+                    layout, q_ptr, ldq, k_ptr if keys else 0, ldk, dpool.data_ptr(), blocks, T, nh, nkv, d, G.stream_ptr())
+    torch.cuda.synchronize()
+    after, pool_after = host(x), host(dpool)
+    live = (pos >= 0) & (pos < max_pos)
+    heads = qkv[:, :width].reshape(T, -1, d)
+    c, s = cos[np.where(live, pos, 0)].astype(np.float64)[:, None], sin[np.where(live, pos, 0)].astype(np.float64)[:, None]
+    ref = rotate(heads[:, :nh + nkv].astype(np.float64), c, s, rot, layout)
+    part = np.abs(heads[:, :nh + nkv]).astype(np.float64)  # |x1| + |x2| bounds both products
+    size = np.abs(part) + np.abs(rotate(part, 0 * c, np.ones_like(s), rot, layout))
+
+    def close(got, want, big):
+        assert np.all(np.abs(got - want) <= BF * np.abs(want) + 3 * F32 * big), np.abs(got - want).max()
+
+    if in_place:
+        close(after[live, :nh * d], ref[live, :nh].reshape(-1, nh * d), size[live, :nh].reshape(-1, nh * d))
+        assert np.array_equal(after[live, (nh + nkv) * d:], qkv[live, (nh + nkv) * d:])
+        if not keys:
+            assert np.array_equal(after[live, nh * d:], qkv[live, nh * d:])
+        got_k = after[:, nh * d:(nh + nkv) * d]
+        assert np.all(np.isnan(after[~live]))
+    else:
+        assert np.array_equal(after, qkv, equal_nan=True)
+        got_q, got_k = host(q_out), host(k_out)
+        close(got_q[:T][live][:, :nh * d], ref[live, :nh].reshape(-1, nh * d), size[live, :nh].reshape(-1, nh * d))
+        rest = np.ones_like(got_q, bool)
+        rest[:T][live, :nh * d] = False
+        assert np.array_equal(got_q[rest], q0[rest])
+        rest = np.ones_like(got_k, bool)
+        if keys:
+            rest[:T][live, :nkv * d] = False
+        assert np.array_equal(got_k[rest], k0[rest])
+        got_k = got_k[:T, :nkv * d]
+    if keys:
+        close(got_k[live], ref[live, nh:].reshape(-1, nkv * d), size[live, nh:].reshape(-1, nkv * d))
+    want = pool.copy()
+    seen = np.ones(pool.shape, bool)
+    for t in np.nonzero(live & (slot >= 0) & (slot < blocks * BLOCK))[0]:
+        p, o = slot[t] // BLOCK, slot[t] % BLOCK
+        close(pool_after[p, 0, :, o], ref[t, nh:], size[t, nh:])
+        if keys:
+            assert np.array_equal(pool_after[p, 0, :, o].reshape(-1), got_k[t])
+        want[p, 1, :, o] = heads[t, nh + nkv:]
+        seen[p, 0, :, o] = False
+    assert np.array_equal(pool_after[seen], want[seen])
+
+
+# ---------------------------------------------------------------- attention
+
+class Cache:
+    """Sequences behind one prefix in a shuffled pool. Slots and table entries that no
+    token uses hold NaN and blocks that do not exist."""
+
+    def __init__(self, lens, prefix, nh, nkv, d, seed, std=1.5, extra=0, wild=True):
+        rng = np.random.default_rng(seed)
+        self.lens, self.P, self.nh, self.nkv, self.d, self.B = list(lens), prefix, nh, nkv, d, len(lens)
+        self.max_ctx = max(lens) + extra
+        self.width = -(-max(self.max_ctx, 1) // BLOCK) + 1
+        n_own = [-(-n // BLOCK) for n in lens]
+        n_pre = -(-prefix // BLOCK)
+        self.blocks = sum(n_own) + n_pre + 2
+        perm = rng.permutation(self.blocks)
+        self.pool = np.full((self.blocks, 2, nkv, BLOCK, d), np.nan if wild else 0.0, np.float32)
+        self.pool[:, 1, :, 1::2] = np.inf if wild else 0.0
+        self.prefix = perm[:n_pre].astype(np.int32)
+        self.table = np.full((self.B, self.width), 2 ** 31 - 1 if wild else 0, np.int32)
+        self.table[:, ::2] = -5 if wild else 0
+        at = n_pre
+        for b, n in enumerate(n_own):
+            self.table[b, :n] = perm[at:at + n]
+            at += n
+        self.k = [bf(rng, (prefix + n, nkv, d), std) for n in lens]
+        self.v = [bf(rng, (prefix + n, nkv, d)) for n in lens]
+        for b in range(1, self.B):
+            self.k[b][:prefix], self.v[b][:prefix] = self.k[0][:prefix], self.v[0][:prefix]
+        for t in range(prefix):
+            self._put(self.prefix[t // BLOCK], t % BLOCK, self.k[0][t], self.v[0][t])
+        for b, n in enumerate(lens):
+            for t in range(n):
+                self._put(self.table[b, t // BLOCK], t % BLOCK, self.k[b][prefix + t], self.v[b][prefix + t])
+        self.q = bf(rng, (self.B, nh * d), std)
+        self.ctx = np.array(lens, np.int32)
+
+    def _put(self, block, off, k, v):
+        self.pool[block, 0, :, off], self.pool[block, 1, :, off] = k, v
+
+    def exact(self, b, drop=()):
+        """Output, bounds on its error, probabilities [nh][P + n] and their bound. `drop`: tokens not cached."""
+        g, d, n = self.nh // self.nkv, self.d, self.P + self.lens[b]
+        q = self.q[b].reshape(self.nkv, g, d).astype(np.float64)
+        k, v = self.k[b].astype(np.float64).transpose(1, 2, 0), self.v[b].astype(np.float64).transpose(1, 0, 2)
+        if n == 0:
+            return np.zeros(self.nh * d), np.zeros(self.nh * d), np.zeros((self.nh, 0)), np.zeros((self.nh, 0))
+        s = q @ k / np.sqrt(d)
+        s[:, :, list(drop)] = -np.inf
+        # float32 products and sums of d terms, the scale and the subtraction: their share of a
+        # probability's error, twice (its own and the sum's), with the sum's n additions
+        ds = (d + 8) * F32 * (np.abs(q) @ np.abs(k)).max(axis=2, keepdims=True) / np.sqrt(d)
+        m = s.max(axis=2, keepdims=True)
+        e = np.exp(s - np.where(np.isinf(m), 0, m))
+        tot = e.sum(axis=2, keepdims=True)
+        p = e / np.where(tot == 0, 1, tot)
+        o = p @ v
+        rel = 2 * ds + (n + 16) * F32
+        tol = BF * np.abs(o) + (BF + rel) * (p @ np.abs(v)) + 1e-30
+        return o.reshape(-1), tol.reshape(-1), p.reshape(self.nh, n), (p * rel).reshape(self.nh, n)
+
+    def device(self):
+        return dict(q=dev_bf(self.q), pool=dev_bf(self.pool), prefix=dev(self.prefix), table=dev(self.table), ctx=dev(self.ctx))
+
+
+def run_shared(c, dv=None, ldq=None, ldo=None, stream=None, ws=None):
+    torch = G.torch()
+    hs = _hs()
+    dv = dv or c.device()
+    w = c.nh * c.d
+    ldo = ldo or w
+    out = torch.full((c.B + 1, ldo), 7.0, dtype=torch.bfloat16, device="cuda")
+    nbytes = hs.hs_k_attn_decode_shared_ws(c.B, c.nh, c.nkv, c.d, c.P, c.max_ctx)
+    ws = workspace(nbytes) if ws is None else ws
+    hs.hs_k_attn_decode_shared(dv["q"].data_ptr(), ldq or w, dv["pool"].data_ptr(), c.blocks, dv["prefix"].data_ptr(), c.P,
+                               dv["table"].data_ptr(), dv["ctx"].data_ptr(), out.data_ptr(), ldo, c.B, c.nh, c.nkv, c.d, c.width,
+                               c.max_ctx, ws.data_ptr(), nbytes, G.stream_ptr() if stream is None else stream)
+    torch.cuda.synchronize()
+    return host(out)
+
+
+SHARED = [
+    ([5], 0, 4, 4, 64), ([0], 1, 4, 4, 64), ([1, 0, 20], 77, 4, 4, 64), ([0, 0], 0, 8, 2, 128), ([0, 3], 0, 8, 8, 64),
+    ([17, 128, 129, 0, 1], 16, 32, 8, 128), ([100, 5], 640, 32, 32, 128), ([300, 0, 16, 127], 129, 8, 4, 128),
+    ([33] * 9, 200, 16, 1, 128), ([2, 31], 500, 12, 1, 128), ([40, 7, 64], 333, 6, 2, 64), ([3] * 40, 300, 8, 2, 64),
+    ([0] * 5, 1000, 10, 2, 128), ([700, 1300, 60], 15, 8, 8, 128), ([1, 2, 3] * 11, 513, 20, 4, 128), ([1] * 130, 90, 4, 1, 64),
+    ([5] * 33, 2100, 16, 4, 64), ([64] * 70, 700, 8, 2, 128), ([9, 0, 30], 4100, 4, 4, 128)]
+
+
+@pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED)
+def test_attn_decode_shared(lens, prefix, nh, nkv, d):
+    """Every row within its own rounding bound; a second call gives the same bits; the
+    rows behind the batch stay."""
+    c = Cache(lens, prefix, nh, nkv, d, len(lens) * 1000 + prefix)
+    got = run_shared(c)
+    for b in range(c.B):
+        o, tol, _, _ = c.exact(b)
+        assert np.all(np.abs(got[b] - o) <= tol), (b, np.nanmax(np.abs(got[b] - o) / tol))
+    assert np.all(got[c.B] == 7.0)
+    assert np.array_equal(got, run_shared(c))
+
+
+def test_attn_decode_shared_without_own_caches():
+    """max_ctx 0: no block table, no own tokens anywhere."""
+    torch = G.torch()
+    hs = _hs()
+    c = Cache([0, 0, 0], 130, 8, 2, 128, 3)
+    dv = c.device()
+    out = torch.zeros((3, 8 * 128), dtype=torch.bfloat16, device="cuda")
+    nbytes = hs.hs_k_attn_decode_shared_ws(3, 8, 2, 128, 130, 0)
+    ws = workspace(nbytes)
+    hs.hs_k_attn_decode_shared(dv["q"].data_ptr(), 1024, dv["pool"].data_ptr(), c.blocks, dv["prefix"].data_ptr(), 130, 0,
+                               dv["ctx"].data_ptr(), out.data_ptr(), 1024, 3, 8, 2, 128, 0, 0, ws.data_ptr(), nbytes, G.stream_ptr())
+    torch.cuda.synchronize()
+    for b in range(3):
+        o, tol, _, _ = c.exact(b)
+        assert np.all(np.abs(host(out)[b] - o) <= tol), b
+
+
+def test_attn_decode_shared_strides_and_lengths_outside():
+    """Rows wider than their heads (NaN between them); lengths below 0 and above max_ctx are cut."""
+    c = Cache([20, 45, 45, 0], 50, 8, 2, 64, 11)
+    dv = c.device()
+    wide = np.full((4, 8 * 64 + 40), np.nan, np.float32)
+    wide[:, :8 * 64] = c.q
+    dv["q"] = dev_bf(wide)
+    dv["ctx"] = dev(np.array([20, 45, 1000, -3], np.int32))
+    got = run_shared(c, dv, ldq=wide.shape[1], ldo=8 * 64 + 6)
+    for b in range(4):
+        o, tol, _, _ = c.exact(b)
+        assert np.all(np.abs(got[b, :512] - o) <= tol), b
+    assert np.all(got[:, 512:] == 7.0) and np.all(got[4] == 7.0)
+
+
+def test_attn_decode_shared_blocks_outside_the_pool():
+    """A table entry that names no block of the pool: its tokens count as not cached."""
+    for lens, prefix, nh, nkv in (([40, 200], 70, 8, 2), ([40, 30] * 12, 300, 8, 2), ([10, 70], 300, 4, 4)):
+        c = Cache(lens, prefix, nh, nkv, 128, 5)
+        c.table[1, 1] = c.blocks
+        c.prefix[2] = -1
+        got = run_shared(c)
+        for b in range(c.B):
+            o, tol, _, _ = c.exact(b, list(range(32, 48)) + (list(range(prefix + 16, min(prefix + 32, prefix + c.lens[b]))) if b == 1 else []))
+            assert np.all(np.abs(got[b] - o) <= tol), (lens, b)
+
+
+@pytest.mark.parametrize("what", [np.nan, np.inf])
+def test_attn_decode_shared_non_finite_stays_where_it_is(what):
+    """A NaN or infinite value of one own token reaches its sequence and kv head alone; one in the
+    prefix reaches every sequence, that kv head alone."""
+    for prefix_token in (False, True):
+        c = Cache([40] * 10, 140, 8, 2, 128, 8)
+        if prefix_token:
+            c.pool[c.prefix[3], 1, 1, 5] = what
+        else:
+            c.pool[c.table[4, 1], 1, 1, 5] = what
+        got = run_shared(c)
+        for b in range(10):
+            o, tol, _, _ = c.exact(b)
+            hit = prefix_token or b == 4
+            ok = np.abs(got[b] - o) <= tol
+            assert ok[:512].all() and (not np.isfinite(got[b, 512:]).any() if hit else ok[512:].all()), b
+
+
+def test_attn_decode_shared_large_scores():
+    """Scores of several hundred, largest first, last and in the prefix: no overflow."""
+    c = Cache([70, 3, 0, 150], 200, 8, 4, 64, 21, std=9.0)
+    got = run_shared(c)
+    for b in range(4):
+        o, tol, _, _ = c.exact(b)
+        assert np.all(np.abs(got[b] - o) <= tol), b
+
+
+@pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED[:3] + SHARED[4:14] + [([2000, 1025, 1024], 0, 8, 2, 128), ([1500, 3], 100, 4, 4, 64)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_attn_decode_weights(lens, prefix, nh, nkv, d, in_place):
+    """Outputs as above; weights within the error of G probabilities and of the accumulation;
+    what lies past a sequence's tokens stays; positions of the newest tokens only."""
+    torch = G.torch()
+    hs = _hs()
+    c = Cache(lens, prefix, nh, nkv, d, len(lens) * 77 + prefix, extra=3)
+    rng = np.random.default_rng(9)
+    g, stride, decay = nh // nkv, c.max_ctx + 5, np.float32(0.9)
+    acc = np.exp(rng.standard_normal((c.B, nkv, stride)) * 3).astype(np.float32)
+    for b, n in enumerate(lens):
+        acc[b, :, max(0, n - 1):] = np.nan
+    pos = rng.integers(0, 1000, acc.shape).astype(np.int32)
+    seen = rng.integers(5000, 6000, c.B).astype(np.int32)
+    dv = c.device()
+    dacc, dpos, dseen = dev(acc), dev(pos), dev(seen)
+    dout = dacc if in_place else torch.full_like(dacc, -3.0)
+    out = torch.full((c.B + 1, nh * d), 7.0, dtype=torch.bfloat16, device="cuda")
+    nbytes = hs.hs_k_attn_decode_weights_ws(c.B, nh, nkv, d, prefix, c.max_ctx)
+    ws = workspace(nbytes)
+    hs.hs_k_attn_decode_weights(dv["q"].data_ptr(), nh * d, dv["pool"].data_ptr(), c.blocks, dv["prefix"].data_ptr(), prefix,
+                                dv["table"].data_ptr(), dv["ctx"].data_ptr(), out.data_ptr(), nh * d, dacc.data_ptr(),
+                                dout.data_ptr(), stride, float(decay), dpos.data_ptr(), dseen.data_ptr(), c.B, nh, nkv, d,
+                                c.width, c.max_ctx, ws.data_ptr(), nbytes, G.stream_ptr())
+    torch.cuda.synchronize()
+    got, w, p_after = host(out), host(dout), host(dpos)
+    assert np.all(got[c.B] == 7.0)
+    for b, n in enumerate(lens):
+        o, tol, p, dp = c.exact(b)
+        assert np.all(np.abs(got[b] - o) <= tol), b
+        want = p[:, prefix:].reshape(nkv, g, n).sum(1)
+        bound = dp[:, prefix:].reshape(nkv, g, n).sum(1) + (g + 2) * F32 * want
+        if n:
+            old = acc[b, :, :n - 1].astype(np.float64) * np.float64(decay)
+            want[:, :n - 1] += old
+            bound[:, :n - 1] += 2 * F32 * (old + want[:, :n - 1])
+            assert np.all(np.abs(w[b, :, :n] - want) <= bound + 1e-37), (b, np.abs(w[b, :, :n] - want).max())
+            assert np.all(p_after[b, :, n - 1] == seen[b] - 1)
+        rest = np.ones(pos.shape[1:], bool)
+        if n:
+            rest[:, n - 1] = False
+        assert np.array_equal(p_after[b][rest], pos[b][rest])
+        assert np.all(np.isnan(w[b, :, n:]) if in_place else w[b, :, n:] == -3.0)
+
+
+# ----------------------------------------------------------------- eviction
+
+def evicted(acc, pos, n, seen, keep, sinks, recent):
+    """Slots of one row: which token lies in each of the first min(n, keep)."""
+    held = (pos[:n] < sinks) | (pos[:n].astype(np.int64) >= int(seen) - recent)
+    a = np.where(np.isnan(acc[:n]), -np.inf, acc[:n]).astype(np.float64)
+    order = sorted(range(n), key=lambda t: (not held[t], 0 if held[t] else bool(np.isnan(acc[t])), 0 if held[t] else -a[t], t))
+    best = set(order[:keep])
+    slots = list(range(min(n, keep)))
+    late = [t for t in range(keep, n) if t in best]
+    for t in [t for t in slots if t not in best]:
+        slots[t] = late.pop(0)
+    return slots
+
+
+EVICT = [([5], 8, 0, 0, 4, 64), ([9, 8, 7, 0, 1], 8, 1, 2, 4, 64), ([33, 40, 2], 1, 0, 0, 2, 128), ([50], 49, 4, 40, 8, 128),
+         ([1023, 1024, 1025, 1026], 1024, 4, 100, 1, 64), ([3000, 2049, 100], 2048, 4, 256, 2, 128), ([5000], 700, 0, 0, 2, 128),
+         ([12000, 11000], 2048, 4, 64, 2, 64), ([300, 260], 100, 70, 70, 3, 64), ([40000], 16, 2, 2, 1, 64), ([17] * 30, 16, 0, 16, 3, 128)]
+
+
+def evict_case(lens, keep, sinks, recent, nkv, d, seed, kind):
+    rng = np.random.default_rng(seed)
+    B, most = len(lens), max(lens)
+    stride, width = most + 3, -(-most // BLOCK) + 1
+    acc = np.exp(rng.standard_normal((B, nkv, stride)) * 2).astype(np.float32)
+    if kind == "ties":
+        acc = rng.integers(0, 3, acc.shape).astype(np.float32) * np.float32(0.5)
+        acc[rng.random(acc.shape) < 0.1] = -0.0
+    if kind == "odd":
+        acc[rng.random(acc.shape) < 0.1] = np.nan
+        acc[rng.random(acc.shape) < 0.1] = np.inf
+        acc[rng.random(acc.shape) < 0.1] = -np.inf
+        acc *= rng.choice([-1.0, 1.0, 1e-42], acc.shape).astype(np.float32)
+    pos = np.stack([np.stack([rng.permutation(stride * 2)[:stride] for _ in range(nkv)]) for _ in range(B)]).astype(np.int32)
+    seen = np.array([2 * stride - 5] * B, np.int32)
+    own = sum(-(-n // BLOCK) for n in lens)
+    perm, at = rng.permutation(own + 2), 0
+    table = np.full((B, width), 2 ** 31 - 1, np.int32)
+    for b, n in enumerate(lens):
+        m = -(-n // BLOCK)
+        table[b, :m] = perm[at:at + m]
+        at += m
+    pool = rng.integers(0, 0x7F00, (own + 2, 2, nkv, BLOCK, d)).astype(np.uint16)
+    return acc, pos, seen, table, pool, stride, width
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("kind", ["plain", "ties", "odd"])
+@pytest.mark.parametrize("lens,keep,sinks,recent,nkv,d", EVICT)
+def test_kv_evict(lens, keep, sinks, recent, nkv, d, kind, in_place):
+    """Everything bit for bit: the rows that moved and those that did not, weights and positions,
+    and what is not to be written."""
+    torch = G.torch()
+    hs = _hs()
+    acc, pos, seen, table, pool, stride, width = evict_case(lens, keep, sinks, recent, nkv, d, sum(lens) + keep, kind)
+    B, most = len(lens), max(lens)
+    kept = min(keep, most)
+    out_stride = stride if in_place else kept + 2
+    dacc, dpos, dseen, dtab = dev(acc), dev(pos), dev(seen), dev(table)
+    dctx = dev(np.array(lens, np.int32))
+    dpool = torch.from_numpy(pool.view(np.int16)).cuda()
+    acc_out = dacc if in_place else torch.full((B, nkv, out_stride), -9.0, dtype=torch.float32, device="cuda")
+    pos_out = dpos if in_place else torch.full((B, nkv, out_stride), -9, dtype=torch.int32, device="cuda")
+    ctx_out = torch.full((B + 1,), -9, dtype=torch.int32, device="cuda")
+    nbytes = hs.hs_k_kv_evict_ws(B, nkv, keep, most)
+    ws = workspace(nbytes)
+    hs.hs_k_kv_evict(dpool.data_ptr(), pool.shape[0], dtab.data_ptr(), dctx.data_ptr(), dseen.data_ptr(), dacc.data_ptr(),
+                     dpos.data_ptr(), stride, acc_out.data_ptr(), pos_out.data_ptr(), out_stride, ctx_out.data_ptr(), keep, sinks,
+                     recent, B, nkv, d, width, most, ws.data_ptr(), nbytes, G.stream_ptr())
+    torch.cuda.synchronize()
+    want_pool = pool.copy()
+    want_acc = acc.copy() if in_place else np.full((B, nkv, out_stride), -9.0, np.float32)
+    want_pos = pos.copy() if in_place else np.full((B, nkv, out_stride), -9, np.int32)
+    for b, n in enumerate(lens):
+        for h in range(nkv):
+            src = np.array(evicted(acc[b, h], pos[b, h], n, seen[b], keep, sinks, recent), int)
+            m = len(src)
+            want_acc[b, h, :m], want_pos[b, h, :m] = acc[b, h, src], pos[b, h, src]
+            to = np.arange(m)
+            want_pool[table[b, to // BLOCK], :, h, to % BLOCK] = pool[table[b, src // BLOCK], :, h, src % BLOCK]
+    assert np.array_equal(host(ctx_out), np.array([min(n, keep) for n in lens] + [-9]))
+    assert np.array_equal(host(pos_out), want_pos)
+    assert np.array_equal(host(acc_out).view(np.int32), want_acc.view(np.int32))
+    assert np.array_equal(dpool.cpu().numpy().view(np.uint16), want_pool)
+
+
+def test_kv_evict_moves_outside_the_pool_are_left_out():
+    torch = G.torch()
+    hs = _hs()
+    n, keep, nkv, d = 200, 100, 2, 64
+    acc, pos, seen, table, pool, stride, width = evict_case([n], keep, 0, 0, nkv, d, 1, "plain")
+    table[0, 2], table[0, 9] = -1, pool.shape[0]
+    dacc, dpos, dseen, dtab, dctx = dev(acc), dev(pos), dev(seen), dev(table), dev(np.array([n], np.int32))
+    dpool = torch.from_numpy(pool.view(np.int16)).cuda()
+    ctx_out = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nbytes = hs.hs_k_kv_evict_ws(1, nkv, keep, n)
+    ws = workspace(nbytes)
+    hs.hs_k_kv_evict(dpool.data_ptr(), pool.shape[0], dtab.data_ptr(), dctx.data_ptr(), dseen.data_ptr(), dacc.data_ptr(),
+                     dpos.data_ptr(), stride, dacc.data_ptr(), dpos.data_ptr(), stride, ctx_out.data_ptr(), keep, 0, 0, 1, nkv, d,
+                     width, n, ws.data_ptr(), nbytes, G.stream_ptr())
+    torch.cuda.synchronize()
+    want = pool.copy()
+    for h in range(nkv):
+        src = evicted(acc[0, h], pos[0, h], n, seen[0], keep, 0, 0)
+        for t, s in enumerate(src):
+            if t // BLOCK != 2 and s // BLOCK != 9 and t != s:
+                want[table[0, t // BLOCK], :, h, t % BLOCK] = pool[table[0, s // BLOCK], :, h, s % BLOCK]
+    assert np.array_equal(dpool.cpu().numpy().view(np.uint16), want)
+
+
+# ----------------------------------------------------------------- together
+
+class Budget:
+    """A batch under a cache budget behind a shared prefix: the state of the operators' run,
+    one decode step's calls, and the same step in float64 on the host."""
+
+    def __init__(self, nh, nkv, d, lens, prefix, keep, seed):
+        self.c = Cache(lens, prefix, nh, nkv, d, seed, wild=False)
+        c, rng = self.c, np.random.default_rng(seed + 1)
+        torch = G.torch()
+        self.hs, self.keep, self.sinks, self.recent = _hs(), keep, 2, 8
+        self.rot, self.max_pos, self.decay = d // 2, 4096, 0.9375
+        self.cap = keep + 1          # tokens of a sequence between two evictions
+        assert max(lens) <= keep
+        self.width = -(-self.cap // BLOCK)
+        self.blocks = c.blocks + c.B * self.width
+        pool = np.zeros((self.blocks, 2, nkv, BLOCK, d), np.float32)
+        pool[:c.blocks] = c.pool
+        self.table = c.blocks + rng.permutation(c.B * self.width).reshape(c.B, self.width).astype(np.int32)
+        acc = np.zeros((c.B, nkv, self.cap), np.float32)
+        pos = np.zeros((c.B, nkv, self.cap), np.int32)
+        for b, n in enumerate(lens):
+            for t in range(n):
+                pool[self.table[b, t // BLOCK], :, :, t % BLOCK] = np.stack([c.k[b][prefix + t], c.v[b][prefix + t]])
+            acc[b, :, :n] = np.exp(rng.standard_normal((nkv, n)))
+            pos[b, :, :n] = np.arange(n)
+        self.pool, self.acc, self.pos = dev_bf(pool), dev(acc), dev(pos)
+        self.ctx = dev(np.array(lens, np.int32))
+        self.seen = dev(np.array(lens, np.int32))
+        self.next_ctx = torch.zeros_like(self.ctx)
+        self.dtable, self.prefix = dev(self.table), dev(c.prefix)
+        self.slot, self.at = torch.zeros_like(self.ctx), torch.zeros_like(self.ctx)
+        self.row = torch.arange(c.B, device="cuda")
+        self.cos = torch.zeros((self.max_pos, self.rot // 2), dtype=torch.float32, device="cuda")
+        self.sin = torch.zeros_like(self.cos)
+        self.qkv = dev_bf(np.zeros((c.B, (nh + 2 * nkv) * d), np.float32))
+        self.q = dev_bf(np.zeros((c.B, nh * d), np.float32))
+        self.out = dev_bf(np.zeros((c.B, nh * d), np.float32))
+        self.ws_w = self.hs.hs_k_attn_decode_weights_ws(c.B, nh, nkv, d, prefix, self.cap)
+        self.ws_e = self.hs.hs_k_kv_evict_ws(c.B, nkv, keep, self.cap)
+        self.w1, self.w2 = workspace(self.ws_w), workspace(self.ws_e)
+        self.hs.hs_k_rope_tables(self.cos.data_ptr(), self.sin.data_ptr(), self.max_pos, self.rot, 10000.0,
+                                 self.hs.rope_scaling("yarn", factor=4.0, original_ctx=1024), G.stream_ptr())
+
+    def step(self):
+        """One decode step from self.qkv to self.out on the current stream."""
+        torch = G.torch()
+        c, hs, s = self.c, self.hs, G.stream_ptr()
+        # the new token goes to slot ctx; its position counts all tokens, the prefix's too
+        self.at.copy_(self.seen + c.P)
+        self.slot.copy_(self.dtable[self.row, torch.div(self.ctx, 16, rounding_mode="floor").long()] * 16 + self.ctx % 16)
+        self.ctx.add_(1)
+        self.seen.add_(1)
+        hs.hs_k_rope_kv(self.qkv.data_ptr(), self.qkv.shape[1], self.at.data_ptr(), self.slot.data_ptr(), self.cos.data_ptr(),
+                        self.sin.data_ptr(), self.max_pos, self.rot, "half", self.q.data_ptr(), c.nh * c.d, 0, 0,
+                        self.pool.data_ptr(), self.blocks, c.B, c.nh, c.nkv, c.d, s)
+        hs.hs_k_attn_decode_weights(self.q.data_ptr(), c.nh * c.d, self.pool.data_ptr(), self.blocks, self.prefix.data_ptr(), c.P,
+                                    self.dtable.data_ptr(), self.ctx.data_ptr(), self.out.data_ptr(), c.nh * c.d,
+                                    self.acc.data_ptr(), self.acc.data_ptr(), self.cap, self.decay, self.pos.data_ptr(),
+                                    self.seen.data_ptr(), c.B, c.nh, c.nkv, c.d, self.width, self.cap, self.w1.data_ptr(),
+                                    self.ws_w, s)
+        hs.hs_k_kv_evict(self.pool.data_ptr(), self.blocks, self.dtable.data_ptr(), self.ctx.data_ptr(), self.seen.data_ptr(),
+                         self.acc.data_ptr(), self.pos.data_ptr(), self.cap, self.acc.data_ptr(), self.pos.data_ptr(), self.cap,
+                         self.next_ctx.data_ptr(), self.keep, self.sinks, self.recent, c.B, c.nkv, c.d, self.width, self.cap,
+                         self.w2.data_ptr(), self.ws_e, s)
+        self.ctx.copy_(self.next_ctx)
+
+    def state(self):
+        return [x.clone() for x in (self.pool, self.acc, self.pos, self.ctx, self.seen)]
+
+    def restore(self, st):
+        for x, y in zip((self.pool, self.acc, self.pos, self.ctx, self.seen), st):
+            x.copy_(y)
+
+
+@pytest.mark.parametrize("nh,nkv,d,lens,prefix,keep", [(8, 2, 128, [30, 29, 32], 70, 32), (4, 4, 64, [3, 40, 17, 20, 9], 0, 40),
+                                                       (16, 4, 128, [20] * 6, 300, 24)])
+def test_decode_steps_under_a_budget(nh, nkv, d, lens, prefix, keep):
+    """Twelve steps of rotation, append, attention, accumulation and eviction. Each step is checked
+    against float64 from the state that the device had before it (weights near one another may
+    rank either way, so the eviction is held to the device's own weights)."""
+    torch = G.torch()
+    B = Budget(nh, nkv, d, lens, prefix, keep, 4)
+    c, g = B.c, nh // nkv
+    rng = np.random.default_rng(3)
+    w = turns(B.rot, 10000.0, "yarn", 4.0, 1024, 1.0, 32.0)
+    mag = 1 + 0.1 * np.log(4.0)
+    for step in range(12):
+        x = bf(rng, (c.B, (nh + 2 * nkv) * d))
+        B.qkv.copy_(dev_bf(x))
+        pool0, acc0, pos0, ctx0, seen0 = (host(t) for t in B.state())
+        B.step()
+        torch.cuda.synchronize()
+        q, out, acc1, pos1, ctx1, pool1 = (host(t) for t in (B.q, B.out, B.acc, B.pos, B.ctx, B.pool))
+        heads = x.reshape(c.B, -1, d).astype(np.float64)
+        for b in range(c.B):
+            n, at = ctx0[b] + 1, seen0[b] + prefix
+            cs, sn = (np.float64(f(at * w)) * mag for f in (np.cos, np.sin))
+            ref = rotate(heads[b, :nh + nkv], cs, sn, B.rot, "half")
+            assert np.abs(q[b].reshape(nh, d) - ref[:nh]).max() <= BF * np.abs(ref).max() + 16 * F32 * np.abs(heads).max()
+            new_k = gen.round_to_bf16(ref[nh:].astype(np.float32))
+            slots = np.arange(n)
+            own = pool0[B.table[b, slots // BLOCK], :, :, slots % BLOCK]     # [n][K, V][nkv][d]
+            own[n - 1, 0], own[n - 1, 1] = new_k, x[b].reshape(-1, d)[nh + nkv:]
+            c.k[b], c.v[b] = (np.concatenate([z[:prefix], own[:, j]]) for j, z in ((0, c.k[b]), (1, c.v[b])))
+            c.q[b], c.lens[b] = q[b], n
+            o, tol, p, dp = c.exact(b)
+            # the rotated key's last rounding may fall either way: half a step of the new token's score
+            slack = 2 * BF * np.abs(c.q[b].reshape(nkv, g, d)).sum(2).max() * np.abs(new_k).max() / np.sqrt(d) * 2.0 ** -8
+            assert np.all(np.abs(out[b] - o) <= tol + slack * np.abs(c.v[b]).max()), (step, b)
+            weight = p[:, prefix:].reshape(nkv, g, n).sum(1)
+            weight[:, :n - 1] += acc0[b, :, :n - 1].astype(np.float64) * B.decay
+            bound = dp[:, prefix:].reshape(nkv, g, n).sum(1) + (g + 4) * F32 * weight + g * slack + 1e-30
+            before = pos0[b].copy()
+            before[:, n - 1] = seen0[b]
+            assert ctx1[b] == min(n, keep)
+            for h in range(nkv):
+                where = {int(t): i for i, t in enumerate(before[h, :n])}
+                src = np.array([where[int(t)] for t in pos1[b, h, :ctx1[b]]])
+                assert len(set(src.tolist())) == ctx1[b]
+                assert np.all(np.abs(acc1[b, h, :ctx1[b]] - weight[h, src]) <= bound[h, src]), (step, b, h)
+                gone = sorted(set(range(n)) - set(src.tolist()))
+                for t in gone:  # nothing protected goes, nothing clearly heavier than what stays
+                    assert 2 <= before[h, t] < seen0[b] + 1 - 8
+                    free = [i for i in src if 2 <= before[h, i] < seen0[b] + 1 - 8]
+                    if free:
+                        assert weight[h, t] <= min(weight[h, i] + bound[h, i] for i in free) + bound[h, t]
+                got = pool1[B.table[b, np.arange(ctx1[b]) // BLOCK], :, h, np.arange(ctx1[b]) % BLOCK]
+                assert np.array_equal(got[:, 1], own[src, 1, h])
+                old = src != n - 1
+                assert np.array_equal(got[old, 0], own[src[old], 0, h])
+
+
+def test_budget_steps_captured_on_two_streams():
+    """Two batches' steps captured into graphs of their own and replayed in turn on two streams, with
+    eager work and waits between: every replay gives the eager run's bits."""
+    torch = G.torch()
+    runs = [Budget(8, 2, 128, [30, 29, 32], 70, 32, 4), Budget(4, 4, 64, [3, 40, 17], 300, 40, 5)]
+    rng = np.random.default_rng(6)
+    xs = [[dev_bf(bf(rng, tuple(r.qkv.shape))) for _ in range(4)] for r in runs]
+    want = []
+    for r, x in zip(runs, xs):
+        st, outs = r.state(), []
+        for y in x:
+            r.qkv.copy_(y)
+            r.step()
+            outs.append([t.clone() for t in [r.out] + r.state()])
+        want.append(outs)
+        r.restore(st)
+    torch.cuda.synchronize()
+    streams, graphs, states = [], [], []
+    for r in runs:
+        s = torch.cuda.Stream()
+        states.append(r.state())
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            r.step()  # warm
+        s.synchronize()
+        r.restore(states[-1])
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            r.step()
+        r.restore(states[-1])
+        streams.append(s)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for i in range(4):
+        for r, x, s, g in zip(runs, xs, streams, graphs):
+            with torch.cuda.stream(s):
+                r.qkv.copy_(x[i])
+                g.replay()
+        junk = torch.randn(1 << 20, device="cuda").sum()
+        torch.cuda.synchronize()
+        assert torch.isfinite(junk)
+        for r, outs in zip(runs, want):
+            for a, b in zip([r.out] + r.state(), outs[i]):
+                assert torch.equal(a, b), i
