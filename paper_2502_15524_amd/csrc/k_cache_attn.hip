@@ -1,25 +1,30 @@
 // Decode attention over a paged cache whose sequences share a prefix, and with
 // the weight that every cached token received.
 //
-// A sequence's tokens are the prefix's, then its own. They are taken in slots of
-// whole blocks: slot v of the prefix's blocks, then of the sequence's own; the
-// slots past a block's last token hold nothing. One workgroup takes 128 slots of
-// one (sequence, kv head), two blocks per wave, and leaves for each query head
-// the unnormalised P V, the largest score (log2 domain) and the sum of
-// exp2(score - largest); a second kernel merges the splits and, where weights
-// are asked for, turns the stored scores into probabilities with the merged
-// statistics. All of it in float32; the probabilities are rounded to bf16 for
-// the second matrix product only (an error of half a bf16 step, as the output's
-// own rounding), their sum and the weights are of the unrounded ones.
+// A sequence's tokens are the prefix's, then its own, in slots of whole blocks
+// (the slots past a block's last token hold nothing). They are cut into splits;
+// each leaves for each query head the unnormalised P V, the largest score (log2
+// domain) and the sum of exp2(score - largest); a second kernel merges the splits
+// and, where weights are asked for, turns the stored scores into probabilities
+// with the merged statistics. All of it in float32; the probabilities are rounded
+// to bf16 for the second matrix product only (an error of half a bf16 step, as
+// the output's own rounding), their sum and the weights are of the unrounded ones.
+//
+// Two kinds of workgroup: of 128 slots of one (sequence, kv head), with the G query
+// heads of the kv head as the rows; and of many tokens of the prefix and one kv
+// head, with the G query heads of all sequences as the rows, so that the prefix is
+// read once for the batch.
 #include "hs_device.h"
 #include "hs_kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hs {
 
 namespace {
-constexpr int kSplit = 128;
+constexpr int kChunk = 128, kChunkBlocks = kChunk / 16;  // slots and blocks of a step of a sequence's workgroup
+                                                        // (at most 8 steps: a lane per block)
 typedef short s16x4_v __attribute__((ext_vector_type(4)));
 
 // The block that holds slots 16 j .. 16 j + 15 of sequence b, and how many
@@ -59,9 +64,9 @@ __device__ __forceinline__ void merge_ml(const float* ml, int n, float& M, float
   L = wave_sum(L);
 }
 
-// Splits of sequence b that hold anything.
+// Splits of a sequence that hold anything: those of the prefix, then its own.
 __device__ __forceinline__ int splits_of(const CacheAttnArgs& a, int ctx) {
-  return min(a.splits, (a.lead_blocks * 16 + ctx + kSplit - 1) / kSplit);
+  return min(a.splits, a.prefix_splits + (a.lead_blocks * 16 + ctx + a.own_chunks * kChunk - 1) / (a.own_chunks * kChunk));
 }
 __device__ __forceinline__ int ctx_of(const CacheAttnArgs& a, int b) {
   return min(max(a.ctx[b], 0), a.max_ctx);
@@ -75,119 +80,141 @@ __device__ __forceinline__ int ctx_of(const CacheAttnArgs& a, int b) {
 // V^T fragments come from transposing LDS reads. Keys and values are read in
 // whole rows, all of them requested before the first is used, and staged
 // through the wave's own LDS buffer, the keys first, then the values over them.
-template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void cache_attn_kernel(
-    CacheAttnArgs a, float scale_log2) {
+constexpr int split_lds(int D) { return 4 * 32 * (D + 16) * 2 + 4 * 16 * 2 * 4; }
+
+template <int D, bool LOOP>
+__device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_log2, int split, int kh,
+                                           int b, char* smem) {
   constexpr int KS = D / 32, DT = D / 16, CH = D / 8;
   constexpr int RPL = 64 / CH;    // rows per load instruction
   constexpr int NL = 16 / RPL;    // load instructions per block
   constexpr int LV = D + 16;      // padded row: the transposing reads on distinct banks
-  __shared__ __attribute__((aligned(16))) bf16_t sV[4][32 * LV];
-  __shared__ float s_ml[4][16][2];
   static_assert(16 * D * 4 <= 32 * LV * 2, "a wave's partial fits its buffer");
-  const auto s_acc = [&](int w) { return reinterpret_cast<float*>(sV[w]); };
-
-  const int split = blockIdx.x / a.n_kv_heads, kh = blockIdx.x - split * a.n_kv_heads;
-  const int b = blockIdx.y, G = a.G;
-  const int ctx = ctx_of(a, b);
-  if (split >= splits_of(a, ctx) && split > 0) return;  // uniform across the workgroup
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const auto sV = [&](int w) { return reinterpret_cast<bf16_t*>(smem) + w * 32 * LV; };
+  const auto s_acc = [&](int w) { return reinterpret_cast<float*>(sV(w)); };
+  float(*const s_ml)[16][2] = reinterpret_cast<float(*)[16][2]>(smem + 4 * 32 * LV * 2);
+  const int G = a.G, ctx = ctx_of(a, b), to = a.prefix_splits + split;
+  if (to > 0 && to >= splits_of(a, ctx)) return;  // uniform across the workgroup
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 15, g = lane >> 4;
   const int64_t head_stride = (int64_t)16 * D, kv_stride = a.n_kv_heads * head_stride;
   const bf16_t* qrow = a.q + (int64_t)b * a.ldq + (int64_t)kh * G * D;
   const int crow = lane / CH, cch = lane % CH;
+  const int j0 = split * a.own_chunks * kChunkBlocks;  // the split's first block
+  const int chunks = LOOP ? min(a.own_chunks, (a.lead_blocks + (ctx + 15) / 16 - j0 + kChunkBlocks - 1) / kChunkBlocks) : 1;
 
+  // lane i holds the split's block i (at most 64)
+  const Block mine = block_of(a, b, j0 + lane, ctx);
   Block blk[2];
-  pack8 ck[2][NL], cv[2][NL], qf[KS];
+  pack8 ck[2][NL], cv[2][NL];
+  const auto load = [&](int c) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    blk[t] = block_of(a, b, split * (kSplit / 16) + wave * 2 + t, ctx);
-    const bf16_t* base = a.pool + (int64_t)blk[t].at * 2 * kv_stride + kh * head_stride;
+    for (int t = 0; t < 2; ++t) {
+      const int i = c * kChunkBlocks + wave * 2 + t;
+      blk[t] = Block{__builtin_amdgcn_readlane(mine.at, i), __builtin_amdgcn_readlane(mine.n, i)};
+      const bf16_t* base = a.pool + (int64_t)blk[t].at * 2 * kv_stride + kh * head_stride;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = RPL * i + crow;
-      const bf16_t* krow = base + r * D + cch * 8;
-      ck[t][i] = r < blk[t].n ? ld16_nt(krow) : zero8();
-      cv[t][i] = r < blk[t].n ? ld16_nt(krow + kv_stride) : zero8();
+      for (int i = 0; i < NL; ++i) {
+        const int r = RPL * i + crow;
+        const bf16_t* krow = base + r * D + cch * 8;
+        ck[t][i] = r < blk[t].n ? ld16_nt(krow) : zero8();
+        cv[t][i] = r < blk[t].n ? ld16_nt(krow + kv_stride) : zero8();
+      }
     }
-  }
+  };
+  load(0);
+  pack8 qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
     qf[ks] = fr < G ? ld16(qrow + fr * D + ks * 32 + g * 8) : zero8();
-  bf16_t* sv = sV[wave];
-  pack8 kf[2][KS];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < NL; ++i) st16(sv + (16 * t + RPL * i + crow) * LV + cch * 8, ck[t][i]);
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[t][ks] = ld16(sv + (16 * t + fr) * LV + ks * 32 + g * 8);
-  asm volatile("" ::: "memory");  // the key reads before the value stores (one wave's LDS operations run in order)
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < NL; ++i) st16(sv + (16 * t + RPL * i + crow) * LV + cch * 8, cv[t][i]);
-
-  f32x4_v s[2];
-  float m = -INFINITY;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    s[t] = f32x4_v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[t][ks]), as_bf16x8(qf[ks]), s[t], 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s[t][j] = 4 * g + j < blk[t].n ? s[t][j] * scale_log2 : -INFINITY;
-      m = fmaxf(m, s[t][j]);
-    }
-    // the scores of the sequence's own tokens, for their weights
-    const int own = (split * (kSplit / 16) + wave * 2 + t - a.lead_blocks) * 16;
-    if (a.scores && own >= 0 && own < ctx && fr < G)
-      *reinterpret_cast<f32x4_v*>(a.scores + ((int64_t)b * a.n_heads + kh * G + fr) * a.score_stride + own + 4 * g) = s[t];
-  }
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
-  const float m0 = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s[t][j] = fast_exp2(s[t][j] - m0);
-      l += s[t][j];
-    }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  pack8 pk;
-  pk.w[0] = pack2bf(s[0][0], s[0][1]);
-  pk.w[1] = pack2bf(s[0][2], s[0][3]);
-  pk.w[2] = pack2bf(s[1][0], s[1][1]);
-  pk.w[3] = pack2bf(s[1][2], s[1][3]);
-  const bf16x8_v pf = as_bf16x8(pk);
-  asm volatile("" ::: "memory");  // the value stores before the fragment reads
+  bf16_t* sv = sV(wave);
+  float m_run = -INFINITY, l_run = 0.f;
   f32x4_v o[DT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    const bf16_t* vp = sv + (4 * g + (fr >> 2)) * LV + dt * 16 + 4 * (fr & 3);
-    const s16x4_v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4_v*)(vp));
-    const s16x4_v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4_v*)(vp + 16 * LV));
-    const bf16x8_v vb =
-        __builtin_bit_cast(bf16x8_v, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pf, f32x4_v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4_v{0.f, 0.f, 0.f, 0.f};
+
+  for (int c = 0; c < chunks; ++c) {
+    pack8 kf[2][KS];
+    const int n[2] = {blk[0].n, blk[1].n};
+    // (a wave's LDS operations run in order: the last chunk's fragment reads come first)
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) st16(sv + (16 * t + RPL * i + crow) * LV + cch * 8, ck[t][i]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[t][ks] = ld16(sv + (16 * t + fr) * LV + ks * 32 + g * 8);
+    asm volatile("" ::: "memory");  // the key reads before the value stores
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) st16(sv + (16 * t + RPL * i + crow) * LV + cch * 8, cv[t][i]);
+    if (LOOP && c + 1 < chunks) load(c + 1);  // on its way during this chunk's products
+
+    f32x4_v s[2];
+    float m = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4_v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[t][ks]), as_bf16x8(qf[ks]), s[t], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[t][j] = 4 * g + j < n[t] ? s[t][j] * scale_log2 : -INFINITY;
+        m = fmaxf(m, s[t][j]);
+      }
+      // the scores of the sequence's own tokens, for their weights
+      const int own = (j0 + c * kChunkBlocks + wave * 2 + t - a.lead_blocks) * 16;
+      if (a.scores && own >= 0 && own < ctx && fr < G)
+        *reinterpret_cast<f32x4_v*>(a.scores + ((int64_t)b * a.n_heads + kh * G + fr) * a.score_stride + own + 4 * g) = s[t];
+    }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float m_new = fmaxf(m_run, m), m0 = m_new == -INFINITY ? 0.f : m_new;
+    const float corr = fast_exp2(m_run - m0);
+    m_run = m_new;
+    l_run *= corr;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[t][j] = fast_exp2(s[t][j] - m0);
+        l_run += s[t][j];
+      }
+    pack8 pk;
+    pk.w[0] = pack2bf(s[0][0], s[0][1]);
+    pk.w[1] = pack2bf(s[0][2], s[0][3]);
+    pk.w[2] = pack2bf(s[1][0], s[1][1]);
+    pk.w[3] = pack2bf(s[1][2], s[1][3]);
+    const bf16x8_v pf = as_bf16x8(pk);
+    asm volatile("" ::: "memory");  // the value stores before the fragment reads
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const bf16_t* vp = sv + (4 * g + (fr >> 2)) * LV + dt * 16 + 4 * (fr & 3);
+      const s16x4_v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4_v*)(vp));
+      const s16x4_v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4_v*)(vp + 16 * LV));
+      const bf16x8_v vb =
+          __builtin_bit_cast(bf16x8_v, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pf, o[dt] * corr, 0, 0, 0);
+    }
   }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
   asm volatile("" ::: "memory");  // the fragment reads before the partial goes over them
   if (fr < G) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
       *reinterpret_cast<f32x4_v*>(s_acc(wave) + fr * D + dt * 16 + 4 * g) = o[dt];
     if (g == 0) {
-      s_ml[wave][fr][0] = l == 0.f ? -INFINITY : m0;  // only NaN scores: a sum, of NaN, without a largest
-      s_ml[wave][fr][1] = l;
+      // (only NaN scores: a sum, of NaN, without a largest)
+      s_ml[wave][fr][0] = m_run == -INFINITY && l_run != 0.f ? 0.f : m_run;
+      s_ml[wave][fr][1] = l_run;
     }
   }
   __syncthreads();
@@ -205,7 +232,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void c
       L += s_ml[w][gg][1] * f;
       O += s_acc(w)[gg * D + d] * f;
     }
-    const int64_t row = ((int64_t)b * a.n_heads + kh * G + gg) * a.splits + split;
+    const int64_t row = ((int64_t)b * a.n_heads + kh * G + gg) * a.splits + to;
     a.part_o[row * D + d] = O;
     if (d == 0) {
       a.part_ml[row * 2] = M;
@@ -214,29 +241,300 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void c
   }
 }
 
-// The output of one (query head, sequence): 256 threads, four splits at a time.
+// Rows of 32 query heads on the columns of 32x32x16 MFMAs, keys on the rows: lane
+// (q, hi) = (lane % 32, lane / 32) gets row q's scores of keys 8 (i / 4) + 4 hi + i % 4
+// (i = 0 .. 15) of 32, which are the second product's B operand as they are. The four
+// waves are RW groups of 32 rows by TW = 4 / RW groups of 32 keys of a step. Keys and
+// values go from memory straight into a ring of NST stages of 32 TW keys, the
+// request of a step NST - 1 steps ahead of its use; each copy covers rows of one cache
+// block, and reads zeros past the block's last token or for a block outside the
+// pool. The 16-byte chunks of a row are XOR-swizzled so that the fragment reads
+// and the transposing reads of the values take different banks.
+template <int D>
+__device__ __forceinline__ int key_swz(int key) {
+  return key & (D / 8 - 1);
+}
+template <int D>
+__device__ __forceinline__ int value_swz(int key) {
+  if constexpr (D == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
+  else return ((key & 3) << 1) | ((key >> 2) & 1);
+}
+constexpr int kPrefixBlocks = 256;  // of one workgroup at most
+constexpr int prefix_stages(int D, int RW) { return D == 128 ? (RW == 4 ? 4 : 2) : (RW == 4 ? 6 : 4); }
+constexpr int prefix_lds(int D, int RW) {
+  return prefix_stages(D, RW) * (4 / RW) * 32 * D * 4 + (kPrefixBlocks + 32) * 4;
+}
+
+template <int D, int RW>
+__device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_log2, int split, int tile,
+                                            int kh, char* smem) {
+  constexpr int TW = 4 / RW, KB = 32 * TW, NST = prefix_stages(D, RW);
+  constexpr int CH = D / 8, ROW = D * 2, BLK = KB * ROW, STG = 2 * BLK;
+  constexpr int KPI = 64 / CH, PER = KB / KPI / 4;  // keys per copy; copies per wave, operand and step
+  static_assert(PER >= 1 && PER * KPI * 4 == KB && 16 % KPI == 0, "copies stay within a block");
+  static_assert(TW == 1 || RW * 32 * D * 4 + RW * 256 <= NST * STG, "the token groups' merge fits the ring");
+  int* const s_blocks = reinterpret_cast<int*>(smem + NST * STG);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % RW, tw = wave / RW;
+  const int q = lane & 31, hi = lane >> 5;
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)smem;
+
+  const int t0 = split * a.prefix_tokens, len = min(a.prefix_tokens, a.prefix_len - t0);
+  const int steps = (len + KB - 1) / KB;
+  for (int i = tid; i < kPrefixBlocks + 32; i += 256) {
+    const int p = 16 * i < len ? a.prefix[t0 / 16 + i] : -1;
+    s_blocks[i] = p >= 0 && p < a.pool_blocks ? p : -1;
+  }
+  // this lane's row
+  const int G = a.G, row = (tile * RW + rw) * 32 + q, rows = a.B * G;
+  const bool real = row < rows;
+  const int rb = row / G, rh = kh * G + row - rb * G;
+  bf16x8_v qf[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+    qf[ks] = as_bf16x8(real ? ld16(a.q + (int64_t)rb * a.ldq + rh * D + ks * 16 + hi * 8) : zero8());
+  // (waited for here: left to their first use, in the loop, the wait would drain the copies)
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
+  __syncthreads();
+
+  int ko[PER], vo[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int key = (PER * wave + i) * KPI + lane / CH, at = lane % CH;
+    ko[i] = (key & 15) * ROW + ((at ^ key_swz<D>(key)) * 16);
+    vo[i] = (key & 15) * ROW + ((at ^ value_swz<D>(key)) * 16);
+  }
+  const int64_t head_bytes = 16ll * ROW, kv_bytes = a.n_kv_heads * head_bytes;
+  const char* const base = reinterpret_cast<const char*>(a.pool) + kh * head_bytes;
+  auto tokens_in = [&](int i) {  // of the workgroup's block i
+    const int p = __builtin_amdgcn_readfirstlane(s_blocks[i]);
+    return p < 0 ? 0 : min(16, len - 16 * i);
+  };
+  auto request = [&](int step) {
+    const uint32_t to = lds0 + (step % NST) * STG + wave * PER * 1024;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = (step * KB + (PER * wave + i) * KPI) / 16;
+      const int p = __builtin_amdgcn_readfirstlane(s_blocks[at]);
+      const char* kp = base + (int64_t)max(p, 0) * 2 * kv_bytes;
+      const uint32_t bytes = p < 0 ? 0u : (uint32_t)min(16, len - 16 * at) * ROW;
+      dma16(buf_rsrc(kp, bytes), ko[i], to + i * 1024);
+      dma16(buf_rsrc(kp + kv_bytes, bytes), vo[i], to + BLK + i * 1024);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < NST - 1; ++i) request(i);
+
+  int ka[D / 16], va[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+    ka[ks] = (32 * tw + q) * ROW + (((2 * ks + hi) ^ key_swz<D>(q)) * 16);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int key = 8 * u + 4 * hi + ((lane & 15) >> 2);
+      const int chunk = dt * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      va[dt][u] = BLK + (32 * tw + key) * ROW + ((chunk ^ value_swz<D>(key)) * 16) + (lane & 1) * 8;
+    }
+  f32x16_v o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const bool busy = (tile * RW + rw) * 32 < rows;  // of the wave
+
+  for (int k = 0; k < steps; ++k) {
+    // this wave's copies of step k have landed (those of the NST - 2 steps after it may be
+    // on their way), its reads of step k - 1 are complete; with everybody's at the
+    // barrier the stage of step k - 1 takes the next request
+    if constexpr (PER * 2 * (NST - 2) == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER * 2 * (NST - 2)) : "memory");
+    asm volatile("s_barrier" ::: "memory");
+    request(k + NST - 1);
+    if (!busy) continue;
+    const char* st = smem + (k % NST) * STG;
+    f32x16_v s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ld16(st + ka[ks])), qf[ks], s, 0, 0, 0);
+    const int blk = (k * KB + 32 * tw) / 16, n0 = tokens_in(blk), n1 = tokens_in(blk + 1);
+    if (n0 < 16 || n1 < 16) {  // uniform: blocks that are not full
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if ((8 * (e >> 2) & 15) + 4 * hi + (e & 3) >= (e < 8 ? n0 : n1)) s[e] = -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale_log2;
+    }
+    const float m_new = fmaxf(m_run, mx);
+    const float m0 = m_new == -INFINITY ? 0.f : m_new;
+    if (__any(m_new != m_run)) {
+      const float corr = fast_exp2(m_run - m0);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] *= corr;
+    }
+    float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = fast_exp2(__builtin_fmaf(s[e], scale_log2, -m0));
+      ps[e & 3] += s[e];
+    }
+    l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      pack8 pb;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pb.w[w] = pack2bf(s[8 * h + 2 * w], s[8 * h + 2 * w + 1]);
+      const bf16x8_v pf = as_bf16x8(pb);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const s16x4_v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4_v*)(st + va[dt][0] + h * 16 * ROW));
+        const s16x4_v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4_v*)(st + va[dt][1] + h * 16 * ROW));
+        const bf16x8_v vb =
+            __builtin_bit_cast(bf16x8_v, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb, pf, o[dt], 0, 0, 0);
+      }
+    }
+  }
+  {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+    l_run = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (m_run == -INFINITY && l_run != 0.f) m_run = 0.f;  // only NaN scores
+  if constexpr (TW == 2) {
+    // the second token group's part goes to the first through the ring, which the
+    // copies past the last step (they read nothing) have left
+    float* const s_o = reinterpret_cast<float*>(smem);
+    float* const s_ml = s_o + RW * 32 * D;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tw == 1) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4) =
+              f32x4_v{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+      if (hi == 0) {
+        s_ml[(rw * 32 + q) * 2] = m_run;
+        s_ml[(rw * 32 + q) * 2 + 1] = l_run;
+      }
+    }
+    __syncthreads();
+    if (tw == 1) return;
+    const float m1 = s_ml[(rw * 32 + q) * 2], l1 = s_ml[(rw * 32 + q) * 2 + 1];
+    const float m = fmaxf(m_run, m1);
+    const float c0 = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m);
+    const float c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - m);
+    m_run = m;
+    l_run = l_run * c0 + l1 * c1;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4_v p = *reinterpret_cast<const f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][4 * g + e] = o[i][4 * g + e] * c0 + p[e] * c1;
+      }
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy into LDS outlives the workgroup
+  }
+  if (!real) return;
+  const int64_t to = ((int64_t)rb * a.n_heads + rh) * a.splits + split;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4_v*>(a.part_o + to * D + dt * 32 + g * 8 + hi * 4) =
+          f32x4_v{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+  if (hi == 0) {
+    a.part_ml[to * 2] = m_run;
+    a.part_ml[to * 2 + 1] = l_run;
+  }
+}
+
+// Every token through workgroups of one sequence.
+template <int D, bool LOOP>
+__device__ __forceinline__ void attn_sequences(const CacheAttnArgs& a, float scale_log2, int i, char* smem) {
+  const int per = a.n_kv_heads * a.own_splits, b = i / per, r = i - b * per;
+  attn_split<D, LOOP>(a, scale_log2, r / a.n_kv_heads, r % a.n_kv_heads, b, smem);
+}
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void cache_attn_kernel(
+    CacheAttnArgs a, float scale_log2) {
+  __shared__ __attribute__((aligned(16))) char smem[split_lds(D)];
+  attn_sequences<D, false>(a, scale_log2, blockIdx.x, smem);
+}
+// The prefix's workgroups first (the longest), then the sequences'.
+template <int D, int RW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void cache_attn_shared_kernel(
+    CacheAttnArgs a, float scale_log2) {
+  __shared__ __attribute__((aligned(1024))) char smem[prefix_lds(D, RW) > split_lds(D) ? prefix_lds(D, RW) : split_lds(D)];
+  const int tiles = (a.B * a.G + 32 * RW - 1) / (32 * RW);
+  const int i = blockIdx.x, first = a.prefix_splits * tiles * a.n_kv_heads;
+  if (i < first) {
+    const int j = i / a.n_kv_heads;
+    return attn_prefix<D, RW>(a, scale_log2, j / tiles, j % tiles, i % a.n_kv_heads, smem);
+  }
+  attn_sequences<D, true>(a, scale_log2, i - first, smem);
+}
+
+// The output of one (query head, sequence). A row of 16-byte loads takes D / 4 lanes, so
+// the four waves take 4 * 256 / D splits at a time, up to 64 with all loads in flight (they
+// do not wait for the statistics; rows past the last split re-read it, with weight 0).
 template <int D>
 __device__ __forceinline__ void merge_out(const CacheAttnArgs& a, int h, int b) {
-  constexpr int W = 256 / D;
-  __shared__ float s_o[256];
+  constexpr int LPR = D / 4, RPP = 64 / LPR, U = 16 / RPP;  // lanes per row, rows per wave and load, loads
+  __shared__ f32x4_v s_o[4][LPR];
   const int ctx = ctx_of(a, b), n = splits_of(a, ctx);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = ((int64_t)b * a.n_heads + h) * a.splits;
   const float* ml = a.part_ml + row * 2;
+  f32x4_v o = {0.f, 0.f, 0.f, 0.f};
   float M, L;
-  merge_ml(ml, n, M, L);
-  const int d = threadIdx.x % D, w = threadIdx.x / D;
-  float o = 0.f;
-  for (int s = w; s < n; s += W) {
-    const float m = ml[2 * s];
-    if (m != -INFINITY) o += a.part_o[(row + s) * D + d] * fast_exp2(m - M);
-  }
-  s_o[threadIdx.x] = o;
-  __syncthreads();
-  if (w) return;
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    f32x4_v v[U];
 #pragma unroll
-  for (int i = 1; i < W; ++i) o += s_o[i * D + d];
+    for (int u = 0; u < U; ++u) {
+      const int s = min(s0 + (4 * u + wave) * RPP + lane / LPR, n - 1);
+      v[u] = *reinterpret_cast<const f32x4_v*>(a.part_o + (row + s) * D + (lane % LPR) * 4);
+    }
+    const float m = s0 + lane < n ? ml[2 * (s0 + lane)] : -INFINITY;
+    if (s0 == 0) merge_ml(ml, n, M, L);
+    const float w = m == -INFINITY ? 0.f : fast_exp2(m - M);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float x = __shfl(w, (4 * u + wave) * RPP + lane / LPR, 64);
+      if (x != 0.f) o += v[u] * x;  // (a split without weight may hold anything)
+    }
+  }
+#pragma unroll
+  for (int e = LPR; e < 64; e <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], e, 64);
+  if (lane < LPR) s_o[wave][lane] = o;
+  __syncthreads();
+  if (threadIdx.x >= LPR) return;
+  o = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
   // no token at all, or none with a score above -inf: zero
-  a.out[(int64_t)b * a.ldo + h * D + d] = f2bf(L == 0.f ? 0.f : o / L);
+  const float r = n == 0 || L == 0.f ? 0.f : 1.f / L;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + (int64_t)b * a.ldo + h * D) + lane * 2;
+  out[0] = pack2bf(o[0] * r, o[1] * r);
+  out[1] = pack2bf(o[2] * r, o[3] * r);
 }
 
 // What a sequence's own tokens received: 1024 tokens of one kv head.
@@ -255,7 +553,10 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int 
   __syncthreads();
   const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
   const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
-  for (int t = t0 + threadIdx.x; t < min(t0 + 1024, ctx); t += 256) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = t0 + i * 256 + threadIdx.x;
+    if (t >= ctx) break;
     float p = 0.f;
     for (int gg = 0; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_m[gg]) * s_r[gg];
     if (t == ctx - 1) {
@@ -278,8 +579,26 @@ __global__ __launch_bounds__(256) void cache_attn_merge_kernel(CacheAttnArgs a) 
 CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t D,
                               int64_t prefix_len, int64_t max_ctx, bool weights) {
   CacheAttnPlan p;
-  p.lead_blocks = (int)((prefix_len + 15) / 16);
-  p.splits = std::max<int64_t>(1, (p.lead_blocks * 16ll + max_ctx + kSplit - 1) / kSplit);
+  const int64_t rows = B * (n_heads / n_kv_heads), blocks = (prefix_len + 15) / 16;
+  p.shared = B > 1 && prefix_len > 0 && blocks * 16 + max_ctx > kChunk;
+  p.row_groups = rows > 64 ? 4 : 2;
+  p.lead_blocks = p.shared ? 0 : (int)blocks;
+  p.own_chunks = 1;
+  p.prefix_tokens = 0;
+  p.prefix_splits = 0;
+  if (p.shared) {
+    // Every split costs the batch a partial result (520 bytes per query head at D = 128, written
+    // and read), so a split is as long as leaves 256 workgroups to the prefix, one per CU, and to
+    // the sequences.
+    const int64_t tiles = (rows + 32 * p.row_groups - 1) / (32 * p.row_groups);
+    p.prefix_tokens = (int)std::min<int64_t>(
+        kPrefixBlocks * 16, std::max<int64_t>(128, (prefix_len * n_kv_heads * tiles / 256 + 63) / 64 * 64));
+    p.prefix_splits = (prefix_len + p.prefix_tokens - 1) / p.prefix_tokens;
+    p.own_chunks = (int)std::min<int64_t>(4, std::max<int64_t>(1, B * n_kv_heads * ((max_ctx + kChunk - 1) / kChunk) / 256));
+  }
+  p.own_splits = (p.lead_blocks * 16ll + max_ctx + p.own_chunks * kChunk - 1) / (p.own_chunks * kChunk);
+  if (!p.shared) p.own_splits = std::max<int64_t>(1, p.own_splits);
+  p.splits = p.prefix_splits + p.own_splits;
   p.score_stride = weights ? (max_ctx + 15) / 16 * 16 : 0;
   p.part_o = 0;
   p.part_ml = p.part_o + B * n_heads * p.splits * D;
@@ -294,23 +613,34 @@ hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStr
       (a.ldq % 8) || a.B > 65535 || p.splits < 1)
     return hipErrorInvalidValue;
   const int chunks = a.acc_out ? (a.max_ctx + 1023) / 1024 : 0;
-  const int64_t gx = p.splits * a.n_kv_heads, gm = a.n_heads + (int64_t)chunks * a.n_kv_heads;
+  const int64_t tiles = ((int64_t)a.B * a.G + 32 * p.row_groups - 1) / (32 * p.row_groups);
+  const int64_t gx = (p.prefix_splits * tiles + a.B * p.own_splits) * a.n_kv_heads;
+  const int64_t gm = a.n_heads + (int64_t)chunks * a.n_kv_heads;
   if (gx >= (1ll << 31) || gm >= (1ll << 31)) return hipErrorInvalidValue;
   a.lead_blocks = p.lead_blocks;
+  a.prefix_tokens = p.prefix_tokens;
+  a.prefix_splits = (int)p.prefix_splits;
+  a.own_chunks = p.own_chunks;
+  a.own_splits = (int)p.own_splits;
   a.splits = (int)p.splits;
   a.part_o = ws + p.part_o;
   a.part_ml = ws + p.part_ml;
   a.scores = p.score_stride ? ws + p.scores : nullptr;
   a.score_stride = p.score_stride;
   const float sl = (float)(1.4426950408889634 / sqrt((double)a.D));
-  const dim3 grid((unsigned)gx, a.B), merge((unsigned)gm, a.B);
-  if (a.D == 128) {
-    hipLaunchKernelGGL(cache_attn_kernel<128>, grid, dim3(256), 0, s, a, sl);
-    hipLaunchKernelGGL(cache_attn_merge_kernel<128>, merge, dim3(256), 0, s, a);
-  } else {
-    hipLaunchKernelGGL(cache_attn_kernel<64>, grid, dim3(256), 0, s, a, sl);
-    hipLaunchKernelGGL(cache_attn_merge_kernel<64>, merge, dim3(256), 0, s, a);
-  }
+  const dim3 grid((unsigned)gx), merge((unsigned)gm, a.B);
+  const auto launch = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    if (!p.shared)
+      hipLaunchKernelGGL(cache_attn_kernel<D>, grid, dim3(256), 0, s, a, sl);
+    else if (p.row_groups == 4)
+      hipLaunchKernelGGL((cache_attn_shared_kernel<D, 4>), grid, dim3(256), 0, s, a, sl);
+    else
+      hipLaunchKernelGGL((cache_attn_shared_kernel<D, 2>), grid, dim3(256), 0, s, a, sl);
+    hipLaunchKernelGGL(cache_attn_merge_kernel<D>, merge, dim3(256), 0, s, a);
+  };
+  if (a.D == 128) launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 64>{});
   return hipGetLastError();
 }
 
