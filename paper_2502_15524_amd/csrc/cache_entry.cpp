@@ -120,7 +120,7 @@ extern "C" hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t*
 namespace {
 hs_status cache_attn_sizes(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                            int32_t prefix_len, int32_t max_ctx) {
-  if (B < 1 || B > 65535 || prefix_len < 0 || max_ctx < 0 || prefix_len > 0x7FFFFFF0 || max_ctx > 0x7FFFFFF0)
+  if (B < 1 || B > 65535 || prefix_len < 0 || max_ctx < 0 || prefix_len > 1 << 30 || max_ctx > 1 << 30)
     return fail(HS_EINVAL, "bad arguments");
   return heads_ok(n_heads, n_kv_heads, head_dim);
 }
@@ -228,7 +228,7 @@ extern "C" hs_status hs_k_attn_decode_weights(
 
 namespace {
 hs_status evict_sizes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
-  if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || keep < 1 || max_ctx < 1 || max_ctx > 0x7FFFFFF0)
+  if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || keep < 1 || max_ctx < 1 || max_ctx > 1 << 30)
     return fail(HS_EINVAL, "bad arguments");
   return HS_OK;
 }
@@ -237,7 +237,7 @@ int64_t evict_cap(int32_t keep, int32_t max_ctx) {
   return std::max<int64_t>(0, std::min<int64_t>(keep, (int64_t)max_ctx - keep));
 }
 uint64_t evict_bytes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
-  return 8ull * B * n_kv_heads * evict_cap(keep, max_ctx);
+  return 4ull * B * n_kv_heads * (2 * evict_cap(keep, max_ctx) + 1);
 }
 }  // namespace
 
@@ -265,7 +265,7 @@ extern "C" hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_
     const hs_status r = evict_sizes(B, n_kv_heads, keep, max_ctx);
     if (r != HS_OK) return r;
     if (!pool || !block_table || !ctx || !seen || !acc || !pos || !acc_out || !pos_out || !ctx_out ||
-        pool_blocks < 1 || sinks < 0 || recent < 0 || ctx_out == ctx)
+        pool_blocks < 1 || pool_blocks > 1 << 27 || sinks < 0 || recent < 0 || ctx_out == ctx)
       return fail(HS_EINVAL, "bad arguments");
     if (head_dim != 64 && head_dim != 128) return fail(HS_EINVAL, "head_dim must be 64 or 128");
     if (max_blocks < (max_ctx + 15) / 16) return fail(HS_EINVAL, "block table too narrow");
@@ -281,7 +281,8 @@ extern "C" hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_
     if (w != HS_OK) return w;
     KvEvictArgs a{static_cast<bf16_t*>(pool), pool_blocks, block_table, ctx, seen, acc, pos, stride,
                   acc_out, pos_out, out_stride, ctx_out, keep, sinks, recent, B, n_kv_heads, head_dim,
-                  max_blocks, max_ctx, static_cast<int32_t*>(ws), (int)evict_cap(keep, max_ctx)};
+                  max_blocks, max_ctx, static_cast<int32_t*>(ws), (int)evict_cap(keep, max_ctx), nullptr};
+    a.counts = a.lists + 2ll * B * n_kv_heads * a.cap;
     return done(kv_evict(a, static_cast<hipStream_t>(stream)), "kv_evict");
   } catch (...) {
     return fail(HS_EINVAL, "unexpected internal error");

@@ -213,7 +213,8 @@ struct KvEvictArgs {
   int32_t* ctx_out;                        // [B]
   int keep, sinks, recent;
   int B, n_kv_heads, D, max_blocks, max_ctx;
-  int32_t* lists; int cap;                 // [B][n_kv_heads][2][cap] holes and what fills them
+  int32_t* lists; int cap;                 // [B][n_kv_heads][cap][2] moves: from and to which slot
+  int32_t* counts;                         // [B][n_kv_heads] how many
 };
 hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s);
 

@@ -7,13 +7,24 @@
 // among equal keys. A slot below `keep` whose token goes is a hole; the j-th hole
 // takes the j-th token that stays at or past `keep`: as few rows move as can, the
 // slots of the others do not change, and sources and holes never overlap.
+//
+// One workgroup selects for a row; its time is a chain of round trips and
+// barriers (the weights of 2112 tokens are 17 KB). Rows with few moves move their
+// keys and values there too; those with many leave the moves, as slots of the pool,
+// to a second kernel that spreads the copies, which HBM bounds, over the chip.
 #include "hs_device.h"
 #include "hs_kernels.h"
+
+#include <type_traits>
 
 namespace hs {
 
 namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kCopies = 8;        // of the first pass's histogram, by lane: most weights share a few exponents
+constexpr int kMovesHere = 256;   // per row at most, in the selecting workgroup
+constexpr int kHoles = 4096;      // listed in LDS
+constexpr int kMovesPerGroup = 32;
 
 // Larger keys stay. A NaN is below every weight, a protected token above all.
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int64_t recent_from) {
@@ -23,122 +34,306 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int64
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum of v over the workgroup's threads; *total: of all.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* s_wave, uint32_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t x = v;
+// Sums of the waves' totals before this wave, and of all.
+__device__ __forceinline__ uint32_t waves_before(const uint32_t* s_wave, int wave, uint32_t* all) {
+  uint32_t before = 0, sum = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();  // the last scan's totals have been read
-  if (lane == 63) s_wave[wave] = x;
-  __syncthreads();
-  uint32_t before = 0, all = 0;
+  for (int i = 0; i < kWaves; i += 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(s_wave + i);
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const uint32_t y = s_wave[w];
-    before += w < wave ? y : 0;
-    all += y;
+    for (int j = 0; j < 4; ++j) {
+      before += i + j < wave ? x[j] : 0;
+      sum += x[j];
+    }
   }
-  *total = all;
-  return before + x - v;
+  *all = sum;
+  return before;
+}
+__device__ __forceinline__ int rank_in(uint64_t ballot) {  // set lanes below this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0));
+}
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ uint32_t lane_scan(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast 15: rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast 31: rows 2 and 3
+  return v;
+}
+
+// 16 bytes of a token in slot (block * 16 + offset) of the pool: chunk c of its key (c < D / 8)
+// or value
+template <int D>
+__device__ __forceinline__ bf16_t* chunk_of(const KvEvictArgs& a, int slot, int kh, int c) {
+  constexpr int CH = D / 8;
+  return a.pool + (((int64_t)(slot >> 4) * 2 + c / CH) * a.n_kv_heads + kh) * 16 * D + (slot & 15) * D + c % CH * 8;
+}
+
+// Moves [j0, j1) of a row, four chunks to a thread loaded before the first is stored.
+template <int D, int THREADS>
+__device__ __forceinline__ void move_tokens(const KvEvictArgs& a, const int2* pairs, int j0, int j1, int kh) {
+  constexpr int CH = D / 4, U = 4;  // 16-byte chunks of a token
+  for (int i0 = j0 * CH; i0 < j1 * CH; i0 += U * THREADS) {
+    pack8 v[U];
+    int2 p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * THREADS + threadIdx.x;
+      p[u] = i < j1 * CH ? pairs[i / CH] : make_int2(-1, -1);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p[u].x >= 0) v[u] = ld16_nt(chunk_of<D>(a, p[u].x, kh, (i0 + u * THREADS + threadIdx.x) % CH));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p[u].x >= 0) st16(chunk_of<D>(a, p[u].y, kh, (i0 + u * THREADS + threadIdx.x) % CH), v[u]);
+  }
 }
 }  // namespace
 
-__global__ __launch_bounds__(kThreads) void kv_evict_kernel(KvEvictArgs a) {
-  __shared__ uint32_t s_hist[256], s_wave[kWaves], s_pick[2];
-  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  const int n = min(max(a.ctx[b], 0), a.max_ctx), kept = min(n, a.keep);
+// K > 0: max_ctx is at most K * 1024, and a token's weight, position and key stay in
+// registers (wave w has tokens [64 w per, 64 (w + 1) per), per = ceil(max_ctx / 1024) to a
+// lane; they are requested together with the row's length). K = 0: longer rows, read
+// again in every pass.
+template <int D, int K, bool MOVE>
+__global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a) {
+  constexpr int R = K > 0 ? K : 1;
+  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * kCopies + 3 * 256];
+  __shared__ __attribute__((aligned(16))) uint32_t s_wave[3][kWaves];
+  __shared__ uint32_t s_pick[4][3];
+  __shared__ int s_table[R * 64], s_hole[kHoles];
+  __shared__ int2 s_pair[MOVE ? kMovesHere : 1];
+  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = (int64_t)b * a.n_kv_heads + kh;
   const float* acc = a.acc + row * a.stride;
   const int32_t* pos = a.pos + row * a.stride;
   float* acc_out = a.acc_out + row * a.out_stride;
   int32_t* pos_out = a.pos_out + row * a.out_stride;
-  if (kh == 0 && tid == 0) a.ctx_out[b] = kept;
-  if (n <= a.keep) {
-    for (int t = tid; t < n; t += kThreads) {
-      acc_out[t] = acc[t];
-      pos_out[t] = pos[t];
+  const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
+  float ws[R];
+  int ps[R];
+  int per = (a.max_ctx + kThreads - 1) / kThreads;
+  if constexpr (K > 0) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int t = min(wave * 64 * per + i * 64 + lane, a.max_ctx - 1);
+      ws[i] = acc[t];
+      ps[i] = pos[t];
     }
+    if (tid < R * 64) s_table[tid] = table[min(tid, a.max_blocks - 1)];
+  }
+  const int n = min(max(a.ctx[b], 0), a.max_ctx), kept = min(n, a.keep);
+  const int64_t recent_from = (int64_t)a.seen[b] - a.recent;
+  for (int i = tid; i < 256 * kCopies + 3 * 256; i += kThreads) s_hist[i] = 0;
+  if (kh == 0 && tid == 0) a.ctx_out[b] = kept;
+  if constexpr (K == 0) per = (n + kThreads - 1) / kThreads;
+  const int first = wave * 64 * per + lane;
+  // f(token, weight, position, key) for every token of the lane
+  uint32_t keys[R];
+  if constexpr (K > 0) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) keys[i] = evict_key(ws[i], ps[i], a.sinks, recent_from);
+  }
+  const auto each = [&](auto f) {
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (i < per) f(first + i * 64, ws[i], ps[i], keys[i]);
+    } else {
+      for (int i = 0; i < per; ++i) {
+        const int t = first + i * 64, u = min(t, n - 1);
+        const float w = acc[u];
+        const int p = pos[u];
+        f(t, w, p, evict_key(w, p, a.sinks, recent_from));
+      }
+    }
+  };
+  if (n <= a.keep) {
+    if (!MOVE && tid == 0) a.counts[row] = 0;
+    each([&](int t, float w, int p, uint32_t) {
+      if (t >= n) return;
+      if (acc_out != acc) acc_out[t] = w;
+      if (pos_out != pos) pos_out[t] = p;
+    });
     return;
   }
-  const int64_t recent_from = (int64_t)a.seen[b] - a.recent;
-  const auto key_at = [&](int t) { return evict_key(acc[t], pos[t], a.sinks, recent_from); };
 
   // the keep-th largest key, and how many of the tokens with that key stay
   uint32_t prefix = 0, mask = 0, need = a.keep;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) s_hist[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass, copies = pass ? 1 : kCopies;
+    uint32_t* const hist = s_hist + (pass ? 256 * (kCopies + pass - 1) : 0);
+    each([&](int t, float, int, uint32_t k) {
+      if (t < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & 255) * copies + (lane & (copies - 1))], 1u);
+    });
     __syncthreads();
-    for (int t = tid; t < n; t += kThreads) {
-      const uint32_t k = key_at(t);
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255], 1u);
+    if (wave == 0) {  // lane l has bins 255 - 4 l down to 252 - 4 l
+      uint32_t c[4], sum = 0;
+      if (pass) {
+        const uint4 v = *reinterpret_cast<const uint4*>(hist + 252 - 4 * lane);
+        c[0] = v.w, c[1] = v.z, c[2] = v.y, c[3] = v.x;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          c[j] = 0;
+#pragma unroll
+          for (int i = 0; i < kCopies; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(hist + (255 - 4 * lane - j) * kCopies + i);
+            c[j] += v.x + v.y + v.z + v.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += c[j];
+      const uint32_t above = lane_scan(sum) - sum;
+      if (above < need && above + sum >= need) {  // one lane: its bins hold the key
+        uint32_t left = need - above, j = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (j == (uint32_t)i && c[i] < left) {
+            left -= c[i];
+            ++j;
+          }
+        s_pick[pass][0] = 255 - 4 * lane - j;
+        s_pick[pass][1] = left;
+        s_pick[pass][2] = j == 0 ? c[0] : j == 1 ? c[1] : j == 2 ? c[2] : c[3];
+      }
     }
     __syncthreads();
-    if (tid == 0) {
-      uint32_t left = need;
-      int bin = 255;
-      for (; bin > 0 && s_hist[bin] < left; --bin) left -= s_hist[bin];
-      s_pick[0] = bin;
-      s_pick[1] = left;
-    }
-    __syncthreads();
-    prefix |= s_pick[0] << shift;
+    prefix |= s_pick[pass][0] << shift;
     mask |= 255u << shift;
-    need = s_pick[1];
+    need = s_pick[pass][1];
   }
 
-  // holes and the tokens that fill them, both in slot order
-  int32_t* holes = a.lists + row * 2 * a.cap;
-  int32_t* movers = holes + a.cap;
-  uint32_t eq_seen = 0, n_holes = 0, n_movers = 0;
-  for (int t0 = 0; t0 < n; t0 += kThreads) {
-    const int t = t0 + tid;
-    const uint32_t k = t < n ? key_at(t) : 0u;
-    const bool eq = t < n && k == prefix;
-    uint32_t all;
-    const uint32_t er = eq_seen + block_scan(eq, s_wave, &all);
-    eq_seen += all;
-    const bool stays = t < n && (k > prefix || (eq && er < need));
-    const bool hole = t < a.keep && !stays, mover = t >= a.keep && stays;
-    const uint32_t hr = n_holes + block_scan(hole, s_wave, &all);
-    n_holes += all;
-    const uint32_t mr = n_movers + block_scan(mover, s_wave, &all);
-    n_movers += all;
-    if (hole && hr < (uint32_t)a.cap) holes[hr] = t;
-    if (mover && mr < (uint32_t)a.cap) movers[mr] = t;
-    if (t < a.keep && stays) {
-      acc_out[t] = acc[t];
-      pos_out[t] = pos[t];
-    }
+  // the first `need` of the tokens with that key in slot order stay
+  uint32_t all, eq = 0;
+  const bool ties = s_pick[3][2] != need;  // uniform
+  if (ties) {
+    each([&](int t, float, int, uint32_t k) { eq += __popcll(__ballot(t < n && k == prefix)); });
+    if (lane == 0) s_wave[0][wave] = eq;
+    __syncthreads();
+    eq = waves_before(s_wave[0], wave, &all);
+  }
+  const uint32_t eq0 = eq;
+  const auto stays = [&](uint32_t k, int t) {
+    if (!ties) return t < n && k >= prefix;
+    const bool same = t < n && k == prefix;
+    const uint64_t m = __ballot(same);
+    const bool s = t < n && (k > prefix || (same && eq + rank_in(m) < need));
+    eq += __popcll(m);
+    return s;
+  };
+  uint32_t holes = 0, movers = 0;
+  each([&](int t, float, int, uint32_t k) {
+    const bool s = stays(k, t);
+    holes += __popcll(__ballot(t < a.keep && !s));
+    movers += __popcll(__ballot(t >= a.keep && s));
+  });
+  if (lane == 0) {
+    s_wave[1][wave] = holes;
+    s_wave[2][wave] = movers;
   }
   __syncthreads();
-  const int moves = min((int)n_movers, a.cap);
-  for (int j = tid; j < moves; j += kThreads) {
-    acc_out[holes[j]] = acc[movers[j]];
-    pos_out[holes[j]] = pos[movers[j]];
+  holes = waves_before(s_wave[1], wave, &all);
+  movers = waves_before(s_wave[2], wave, &all);
+  const int moves = min((int)all, a.cap);
+  int2* const pairs = MOVE ? s_pair : reinterpret_cast<int2*>(a.lists) + row * a.cap;
+  const bool in_lds = a.cap <= kHoles;
+  eq = eq0;
+  // the holes' list, and the weights of what keeps its slot
+  each([&](int t, float w, int p, uint32_t k) {
+    const bool s = stays(k, t), hole = t < a.keep && !s;
+    const uint64_t m = __ballot(hole);
+    const uint32_t j = holes + rank_in(m);
+    if (hole && j < (uint32_t)moves) {
+      if (in_lds) s_hole[j] = t;
+      else pairs[j].y = t;
+    }
+    holes += __popcll(m);
+    if (t < a.keep && s) {
+      if (acc_out != acc) acc_out[t] = w;
+      if (pos_out != pos) pos_out[t] = p;
+    }
+  });
+  __syncthreads();
+  const auto slot_of = [&](int t) {
+    const int p = K > 0 ? s_table[t >> 4] : table[t >> 4];
+    return p < 0 || p >= a.pool_blocks ? -1 : p * 16 + (t & 15);
+  };
+  const auto put = [&](int j, int from, int to, float w, int p) {
+    const int x = slot_of(from), y = slot_of(to);
+    acc_out[to] = w;
+    pos_out[to] = p;
+    pairs[j] = x < 0 || y < 0 ? make_int2(-1, -1) : make_int2(x, y);
+  };
+  eq = eq0;
+  each([&](int t, float w, int p, uint32_t k) {
+    const bool mover = stays(k, t) && t >= a.keep;
+    const uint64_t m = __ballot(mover);
+    const uint32_t j = movers + rank_in(m);
+    if (mover && j < (uint32_t)moves) {
+      const int to = in_lds ? s_hole[j] : pairs[j].y;
+      if constexpr (K > 0) {
+        put(j, t, to, w, p);
+      } else {  // other waves may still read the row: in place, nothing of it is written yet
+        pairs[j] = make_int2(t, to);
+      }
+    }
+    movers += __popcll(m);
+  });
+  if constexpr (K == 0) {
+    __syncthreads();
+    for (int j = tid; j < moves; j += kThreads) {
+      const int2 m = pairs[j];
+      put(j, m.x, m.y, acc[m.x], pos[m.x]);
+    }
   }
-  // the moved tokens' keys and values
-  const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
-  const int ch = a.D / 8, per = 2 * ch;
-  for (int i = tid; i < moves * per; i += kThreads) {
-    const int j = i / per, kv = (i % per) / ch, c = i % ch;
-    const int from = movers[j], to = holes[j];
-    const int pf = table[from >> 4], pt = table[to >> 4];
-    if (pf < 0 || pf >= a.pool_blocks || pt < 0 || pt >= a.pool_blocks) continue;
-    const int64_t head = (int64_t)kv * a.n_kv_heads + kh, unit = (int64_t)a.n_kv_heads * 2;
-    st16(a.pool + ((pt * unit + head) * 16 + (to & 15)) * a.D + c * 8,
-         ld16(a.pool + ((pf * unit + head) * 16 + (from & 15)) * a.D + c * 8));
+  if constexpr (MOVE) {
+    __syncthreads();
+    move_tokens<D, kThreads>(a, s_pair, 0, moves, kh);
+  } else {
+    if (tid == 0) a.counts[row] = moves;
   }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void kv_evict_move_kernel(KvEvictArgs a) {
+  const int kh = blockIdx.y, j0 = blockIdx.x * kMovesPerGroup;
+  const int64_t row = (int64_t)blockIdx.z * a.n_kv_heads + kh;
+  const int moves = a.counts[row];
+  if (j0 >= moves) return;
+  move_tokens<D, 256>(a, reinterpret_cast<const int2*>(a.lists) + row * a.cap, j0, min(j0 + kMovesPerGroup, moves), kh);
 }
 
 hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
   if (a.B <= 0) return hipSuccess;
-  if ((a.D != 64 && a.D != 128) || a.n_kv_heads < 1 || a.B > 65535 || a.keep < 1 || a.cap < 0)
+  if ((a.D != 64 && a.D != 128) || a.n_kv_heads < 1 || a.n_kv_heads > 65535 || a.B > 65535 ||
+      a.keep < 1 || a.cap < 0)
     return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kv_evict_kernel, dim3(a.n_kv_heads, a.B), dim3(kThreads), 0, s, a);
+  const dim3 grid(a.n_kv_heads, a.B);
+  const bool here = a.cap <= kMovesHere;
+  const auto launch = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    const auto select = [&](auto k) {
+      constexpr int K = decltype(k)::value;
+      if (here) hipLaunchKernelGGL((kv_evict_select_kernel<D, K, true>), grid, dim3(kThreads), 0, s, a);
+      else hipLaunchKernelGGL((kv_evict_select_kernel<128, K, false>), grid, dim3(kThreads), 0, s, a);  // (no use of D)
+    };
+    if (a.max_ctx <= 4 * kThreads) select(std::integral_constant<int, 4>{});
+    else if (a.max_ctx <= 16 * kThreads) select(std::integral_constant<int, 16>{});
+    else select(std::integral_constant<int, 0>{});
+    if (!here)
+      hipLaunchKernelGGL(kv_evict_move_kernel<D>, dim3((a.cap + kMovesPerGroup - 1) / kMovesPerGroup, a.n_kv_heads, a.B),
+                         dim3(256), 0, s, a);
+  };
+  if (a.D == 128) launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 64>{});
   return hipGetLastError();
 }
 
