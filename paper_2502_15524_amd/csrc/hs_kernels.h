@@ -186,17 +186,17 @@ struct CacheAttnArgs {
   int32_t* pos; const int32_t* seen;       // positions (may be null), tokens seen [B]
   int B, n_heads, n_kv_heads, G, D, max_blocks, max_ctx;
   // set by cache_attn from its plan
-  int lead_blocks, prefix_tokens, prefix_splits, own_chunks, own_splits, splits;
+  int lead_blocks, prefix_tokens, prefix_splits, own_blocks, own_splits, splits;
   float *part_o, *part_ml, *scores;
   int64_t score_stride;
 };
 // How a call is cut, and its workspace (offsets in floats).
 struct CacheAttnPlan {
+  bool direct;                             // a sequence and kv head in one workgroup
   bool shared;                             // the prefix in workgroups of its own
-  int row_groups;                          // of 32 query heads, in each of these
   int lead_blocks;                         // else: prefix blocks before a sequence's own
   int prefix_tokens;                       // per split of the prefix
-  int own_chunks;                          // of 128 slots, per split of a sequence
+  int own_blocks;                          // per split of a sequence
   int64_t prefix_splits, own_splits, splits, score_stride;
   int64_t part_o, part_ml, scores, floats;
 };

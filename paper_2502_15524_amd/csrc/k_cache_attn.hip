@@ -23,8 +23,7 @@
 namespace hs {
 
 namespace {
-constexpr int kChunk = 128, kChunkBlocks = kChunk / 16;  // slots and blocks of a step of a sequence's workgroup
-                                                        // (at most 8 steps: a lane per block)
+constexpr int kDirect = 1024;  // slots that one workgroup takes alone at most
 typedef short s16x4_v __attribute__((ext_vector_type(4)));
 
 // The block that holds slots 16 j .. 16 j + 15 of sequence b, and how many
@@ -48,6 +47,20 @@ __device__ __forceinline__ Block block_of(const CacheAttnArgs& a, int b, int j, 
   return r;
 }
 
+// A buffer descriptor of uniform values, kept in scalar registers.
+__device__ __forceinline__ v4i_t scalar_rsrc(const void* p, uint32_t bytes) {
+  v4i_t r = buf_rsrc(p, bytes);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+  return r;
+}
+
+// 16 bytes read once per call (a non-temporal load)
+__device__ __forceinline__ pack8 ld16_once(__amdgpu_buffer_rsrc_t r, int off) {
+  constexpr int kNonTemporal = 2;
+  return __builtin_bit_cast(pack8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kNonTemporal));
+}
+
 // Merged statistics of a query head of a sequence: the splits' largest score
 // and the sum relative to it. Called by a whole wave; the order is fixed.
 __device__ __forceinline__ void merge_ml(const float* ml, int n, float& M, float& L) {
@@ -66,10 +79,19 @@ __device__ __forceinline__ void merge_ml(const float* ml, int n, float& M, float
 
 // Splits of a sequence that hold anything: those of the prefix, then its own.
 __device__ __forceinline__ int splits_of(const CacheAttnArgs& a, int ctx) {
-  return min(a.splits, a.prefix_splits + (a.lead_blocks * 16 + ctx + a.own_chunks * kChunk - 1) / (a.own_chunks * kChunk));
+  return min(a.splits, a.prefix_splits + (a.lead_blocks + (ctx + 15) / 16 + a.own_blocks - 1) / a.own_blocks);
 }
 __device__ __forceinline__ int ctx_of(const CacheAttnArgs& a, int b) {
   return min(max(a.ctx[b], 0), a.max_ctx);
+}
+// What a token received, added to what it had; the newest starts with it, and gets its position.
+__device__ __forceinline__ void put_weight(const CacheAttnArgs& a, int64_t at, int b, bool newest, float p) {
+  if (newest) {
+    if (a.pos) a.pos[at] = a.seen[b] - 1;
+  } else {
+    p += a.decay * a.acc[at];
+  }
+  a.acc_out[at] = p;
 }
 }  // namespace
 
@@ -80,29 +102,35 @@ __device__ __forceinline__ int ctx_of(const CacheAttnArgs& a, int b) {
 // V^T fragments come from transposing LDS reads. Keys and values are read in
 // whole rows, all of them requested before the first is used, and staged
 // through the wave's own LDS buffer, the keys first, then the values over them.
-constexpr int split_lds(int D) { return 4 * 32 * (D + 16) * 2 + 4 * 16 * 2 * 4; }
+// bytes of LDS: the waves' buffers and statistics, the merged statistics of the direct form
+constexpr int split_lds(int D, int NW) { return NW * 32 * (D + 16) * 2 + (NW + 1) * 16 * 2 * 4; }
 
-template <int D, bool LOOP>
+// NW waves, a step of 32 NW slots; LOOP: as many steps as the split has, else one. DIRECT: the
+// sequence is one split, and the workgroup writes the output and the weights.
+template <int D, int NW, bool LOOP, bool DIRECT = false>
 __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_log2, int split, int kh,
                                            int b, char* smem) {
   constexpr int KS = D / 32, DT = D / 16, CH = D / 8;
   constexpr int RPL = 64 / CH;    // rows per load instruction
   constexpr int NL = 16 / RPL;    // load instructions per block
   constexpr int LV = D + 16;      // padded row: the transposing reads on distinct banks
+  constexpr int CB = 2 * NW;      // blocks of a step
   static_assert(16 * D * 4 <= 32 * LV * 2, "a wave's partial fits its buffer");
   const auto sV = [&](int w) { return reinterpret_cast<bf16_t*>(smem) + w * 32 * LV; };
   const auto s_acc = [&](int w) { return reinterpret_cast<float*>(sV(w)); };
-  float(*const s_ml)[16][2] = reinterpret_cast<float(*)[16][2]>(smem + 4 * 32 * LV * 2);
+  float(*const s_ml)[16][2] = reinterpret_cast<float(*)[16][2]>(smem + NW * 32 * LV * 2);
+  float* const s_fin = reinterpret_cast<float*>(s_ml + NW);  // [16][2]
   const int G = a.G, ctx = ctx_of(a, b), to = a.prefix_splits + split;
-  if (to > 0 && to >= splits_of(a, ctx)) return;  // uniform across the workgroup
+  if (!DIRECT && to > 0 && to >= splits_of(a, ctx)) return;  // uniform across the workgroup
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 15, g = lane >> 4;
   const int64_t head_stride = (int64_t)16 * D, kv_stride = a.n_kv_heads * head_stride;
   const bf16_t* qrow = a.q + (int64_t)b * a.ldq + (int64_t)kh * G * D;
   const int crow = lane / CH, cch = lane % CH;
-  const int j0 = split * a.own_chunks * kChunkBlocks;  // the split's first block
-  const int chunks = LOOP ? min(a.own_chunks, (a.lead_blocks + (ctx + 15) / 16 - j0 + kChunkBlocks - 1) / kChunkBlocks) : 1;
+  const int j0 = split * a.own_blocks;  // the split's first block
+  const int left = a.lead_blocks + (ctx + 15) / 16 - j0;
+  const int chunks = LOOP ? (min(a.own_blocks, left) + CB - 1) / CB : 1;
 
   // lane i holds the split's block i (at most 64)
   const Block mine = block_of(a, b, j0 + lane, ctx);
@@ -111,16 +139,17 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
   const auto load = [&](int c) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int i = c * kChunkBlocks + wave * 2 + t;
+      const int i = c * CB + wave * 2 + t;
       blk[t] = Block{__builtin_amdgcn_readlane(mine.at, i), __builtin_amdgcn_readlane(mine.n, i)};
+      // rows past the block's last token read zeros
       const bf16_t* base = a.pool + (int64_t)blk[t].at * 2 * kv_stride + kh * head_stride;
+      const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, blk[t].n * D * 2, kRsrcWord3);
+      const __amdgpu_buffer_rsrc_t rv =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base + kv_stride), 0, blk[t].n * D * 2, kRsrcWord3);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int r = RPL * i + crow;
-        const bf16_t* krow = base + r * D + cch * 8;
-        ck[t][i] = r < blk[t].n ? ld16_nt(krow) : zero8();
-        cv[t][i] = r < blk[t].n ? ld16_nt(krow + kv_stride) : zero8();
-      }
+      for (int i = 0; i < NL; ++i) ck[t][i] = ld16_once(rk, lane * 16 + i * 1024);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) cv[t][i] = ld16_once(rv, lane * 16 + i * 1024);
     }
   };
   load(0);
@@ -168,7 +197,7 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
         m = fmaxf(m, s[t][j]);
       }
       // the scores of the sequence's own tokens, for their weights
-      const int own = (j0 + c * kChunkBlocks + wave * 2 + t - a.lead_blocks) * 16;
+      const int own = (j0 + c * CB + wave * 2 + t - a.lead_blocks) * 16;
       if (a.scores && own >= 0 && own < ctx && fr < G)
         *reinterpret_cast<f32x4_v*>(a.scores + ((int64_t)b * a.n_heads + kh * G + fr) * a.score_stride + own + 4 * g) = s[t];
     }
@@ -218,25 +247,44 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
     }
   }
   __syncthreads();
-  for (int i = tid; i < G * D; i += 256) {
+  for (int i = tid; i < G * D; i += 64 * NW) {
     const int gg = i / D, d = i % D;
     float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ml[w][gg][0]);
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, s_ml[w][gg][0]);
     float L = 0.f, O = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float mw = s_ml[w][gg][0];
       if (mw == -INFINITY) continue;
       const float f = fast_exp2(mw - M);
       L += s_ml[w][gg][1] * f;
       O += s_acc(w)[gg * D + d] * f;
     }
-    const int64_t row = ((int64_t)b * a.n_heads + kh * G + gg) * a.splits + to;
-    a.part_o[row * D + d] = O;
-    if (d == 0) {
-      a.part_ml[row * 2] = M;
-      a.part_ml[row * 2 + 1] = L;
+    if constexpr (DIRECT) {
+      // no token at all, or none with a score above -inf: zero
+      a.out[(int64_t)b * a.ldo + (kh * G + gg) * D + d] = f2bf(L == 0.f ? 0.f : O / L);
+      if (d == 0) {
+        s_fin[2 * gg] = M == -INFINITY ? 0.f : M;
+        s_fin[2 * gg + 1] = L == 0.f ? 0.f : 1.f / L;
+      }
+    } else {
+      const int64_t row = ((int64_t)b * a.n_heads + kh * G + gg) * a.splits + to;
+      a.part_o[row * D + d] = O;
+      if (d == 0) {
+        a.part_ml[row * 2] = M;
+        a.part_ml[row * 2 + 1] = L;
+      }
+    }
+  }
+  if (DIRECT && a.scores) {
+    __syncthreads();
+    const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
+    const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
+    for (int t = tid; t < ctx; t += 64 * NW) {
+      float p = 0.f;
+      for (int gg = 0; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_fin[2 * gg]) * s_fin[2 * gg + 1];
+      put_weight(a, row + t, b, t == ctx - 1, p);
     }
   }
 }
@@ -244,12 +292,14 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
 // Rows of 32 query heads on the columns of 32x32x16 MFMAs, keys on the rows: lane
 // (q, hi) = (lane % 32, lane / 32) gets row q's scores of keys 8 (i / 4) + 4 hi + i % 4
 // (i = 0 .. 15) of 32, which are the second product's B operand as they are. The four
-// waves are RW groups of 32 rows by TW = 4 / RW groups of 32 keys of a step. Keys and
-// values go from memory straight into a ring of NST stages of 32 TW keys, the
-// request of a step NST - 1 steps ahead of its use; each copy covers rows of one cache
-// block, and reads zeros past the block's last token or for a block outside the
-// pool. The 16-byte chunks of a row are XOR-swizzled so that the fragment reads
-// and the transposing reads of the values take different banks.
+// waves are two groups of 32 rows by two groups of 32 keys of a step. Keys and values go
+// from memory straight into a ring of NST stages of 64 keys, the request of a step
+// NST - 1 steps ahead of its use; a wave's copies of a step cover one cache block, and
+// read zeros past the block's last token or for a block outside the pool. The 16-byte
+// chunks of a row are XOR-swizzled so that the fragment reads and the transposing
+// reads of the values take different banks. Tiles of 64 rows, not 128 with 32 keys a
+// step: the same keys come from L2 for the second tile (8B heads, 32 sequences behind
+// 8192 tokens, MI355X: 26.4 us with 128 rows, 24.1 with 64).
 template <int D>
 __device__ __forceinline__ int key_swz(int key) {
   return key & (D / 8 - 1);
@@ -259,21 +309,19 @@ __device__ __forceinline__ int value_swz(int key) {
   if constexpr (D == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
   else return ((key & 3) << 1) | ((key >> 2) & 1);
 }
-constexpr int kPrefixBlocks = 256;  // of one workgroup at most
-constexpr int prefix_stages(int D, int RW) { return D == 128 ? (RW == 4 ? 4 : 2) : (RW == 4 ? 6 : 4); }
-constexpr int prefix_lds(int D, int RW) {
-  return prefix_stages(D, RW) * (4 / RW) * 32 * D * 4 + (kPrefixBlocks + 32) * 4;
-}
+constexpr int kPrefixBlocks = 64;  // of one workgroup at most: a lane each
+constexpr int kTileRows = 64;
+constexpr int prefix_stages(int D) { return D == 128 ? 2 : 4; }  // 64 KB: two workgroups per CU
+constexpr int prefix_lds(int D) { return prefix_stages(D) * 64 * D * 4; }
 
-template <int D, int RW>
+template <int D>
 __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_log2, int split, int tile,
                                             int kh, char* smem) {
-  constexpr int TW = 4 / RW, KB = 32 * TW, NST = prefix_stages(D, RW);
+  constexpr int RW = kTileRows / 32, KB = 64, NST = prefix_stages(D);
   constexpr int CH = D / 8, ROW = D * 2, BLK = KB * ROW, STG = 2 * BLK;
   constexpr int KPI = 64 / CH, PER = KB / KPI / 4;  // keys per copy; copies per wave, operand and step
-  static_assert(PER >= 1 && PER * KPI * 4 == KB && 16 % KPI == 0, "copies stay within a block");
-  static_assert(TW == 1 || RW * 32 * D * 4 + RW * 256 <= NST * STG, "the token groups' merge fits the ring");
-  int* const s_blocks = reinterpret_cast<int*>(smem + NST * STG);
+  static_assert(PER >= 1 && PER * KPI * 4 == KB && 16 % (PER * KPI) == 0, "a wave's copies stay within a block");
+  static_assert(RW * 32 * D * 4 + RW * 256 <= NST * STG, "the token groups' merge fits the ring");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, tw = wave / RW;
@@ -282,10 +330,9 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
 
   const int t0 = split * a.prefix_tokens, len = min(a.prefix_tokens, a.prefix_len - t0);
   const int steps = (len + KB - 1) / KB;
-  for (int i = tid; i < kPrefixBlocks + 32; i += 256) {
-    const int p = 16 * i < len ? a.prefix[t0 / 16 + i] : -1;
-    s_blocks[i] = p >= 0 && p < a.pool_blocks ? p : -1;
-  }
+  // lane i holds the split's block i (at most 64), -1: none, or none of the pool
+  int mine = 16 * lane < len ? a.prefix[t0 / 16 + lane] : -1;
+  if (mine >= a.pool_blocks) mine = -1;
   // this lane's row
   const int G = a.G, row = (tile * RW + rw) * 32 + q, rows = a.B * G;
   const bool real = row < rows;
@@ -297,7 +344,6 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   // (waited for here: left to their first use, in the loop, the wait would drain the copies)
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
-  __syncthreads();
 
   int ko[PER], vo[PER];
 #pragma unroll
@@ -308,21 +354,21 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   }
   const int64_t head_bytes = 16ll * ROW, kv_bytes = a.n_kv_heads * head_bytes;
   const char* const base = reinterpret_cast<const char*>(a.pool) + kh * head_bytes;
-  auto tokens_in = [&](int i) {  // of the workgroup's block i
-    const int p = __builtin_amdgcn_readfirstlane(s_blocks[i]);
-    return p < 0 ? 0 : min(16, len - 16 * i);
+  auto tokens_in = [&](int i) {  // of the split's block i
+    return __builtin_amdgcn_readlane(mine, i & 63) < 0 ? 0 : min(16, len - 16 * i);
   };
+  // a wave's copies of a step are of one block
   auto request = [&](int step) {
     const uint32_t to = lds0 + (step % NST) * STG + wave * PER * 1024;
+    const int i = (step * KB + PER * wave * KPI) / 16;
+    const int p = __builtin_amdgcn_readlane(mine, i & 63);
+    const char* kp = base + (int64_t)max(p, 0) * 2 * kv_bytes;
+    const uint32_t bytes = p < 0 ? 0u : (uint32_t)max(0, min(16, len - 16 * i)) * ROW;
+    const v4i_t rk = scalar_rsrc(kp, bytes), rv = scalar_rsrc(kp + kv_bytes, bytes);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = (step * KB + (PER * wave + i) * KPI) / 16;
-      const int p = __builtin_amdgcn_readfirstlane(s_blocks[at]);
-      const char* kp = base + (int64_t)max(p, 0) * 2 * kv_bytes;
-      const uint32_t bytes = p < 0 ? 0u : (uint32_t)min(16, len - 16 * at) * ROW;
-      dma16(buf_rsrc(kp, bytes), ko[i], to + i * 1024);
-      dma16(buf_rsrc(kp + kv_bytes, bytes), vo[i], to + BLK + i * 1024);
-    }
+    for (int j = 0; j < PER; ++j) dma16(rk, ko[j], to + j * 1024);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) dma16(rv, vo[j], to + BLK + j * 1024);
   };
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i) request(i);
@@ -357,12 +403,18 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
     request(k + NST - 1);
     if (!busy) continue;
     const char* st = smem + (k % NST) * STG;
+    // (all key fragments are requested before the first product: left to the compiler, each
+    // was read one product ahead, less than an LDS read takes)
+    bf16x8_v kf[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) kf[ks] = as_bf16x8(ld16(st + ka[ks]));
+    __builtin_amdgcn_sched_barrier(0);
     f32x16_v s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ld16(st + ka[ks])), qf[ks], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
     const int blk = (k * KB + 32 * tw) / 16, n0 = tokens_in(blk), n1 = tokens_in(blk + 1);
     if (n0 < 16 || n1 < 16) {  // uniform: blocks that are not full
 #pragma unroll
@@ -415,44 +467,40 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
     l_run = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
   if (m_run == -INFINITY && l_run != 0.f) m_run = 0.f;  // only NaN scores
-  if constexpr (TW == 2) {
-    // the second token group's part goes to the first through the ring, which the
-    // copies past the last step (they read nothing) have left
-    float* const s_o = reinterpret_cast<float*>(smem);
-    float* const s_ml = s_o + RW * 32 * D;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tw == 1) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4) =
-              f32x4_v{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
-      if (hi == 0) {
-        s_ml[(rw * 32 + q) * 2] = m_run;
-        s_ml[(rw * 32 + q) * 2 + 1] = l_run;
-      }
-    }
-    __syncthreads();
-    if (tw == 1) return;
-    const float m1 = s_ml[(rw * 32 + q) * 2], l1 = s_ml[(rw * 32 + q) * 2 + 1];
-    const float m = fmaxf(m_run, m1);
-    const float c0 = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m);
-    const float c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - m);
-    m_run = m;
-    l_run = l_run * c0 + l1 * c1;
+  // the second token group's part goes to the first through the ring, which the
+  // copies past the last step (they read nothing) have left
+  float* const s_o = reinterpret_cast<float*>(smem);
+  float* const s_ml = s_o + RW * 32 * D;
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tw == 1) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_v p = *reinterpret_cast<const f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][4 * g + e] = o[i][4 * g + e] * c0 + p[e] * c1;
-      }
-  } else {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy into LDS outlives the workgroup
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4) =
+            f32x4_v{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+    if (hi == 0) {
+      s_ml[(rw * 32 + q) * 2] = m_run;
+      s_ml[(rw * 32 + q) * 2 + 1] = l_run;
+    }
   }
+  __syncthreads();
+  if (tw == 1) return;
+  const float m1 = s_ml[(rw * 32 + q) * 2], l1 = s_ml[(rw * 32 + q) * 2 + 1];
+  const float m = fmaxf(m_run, m1);
+  const float c0 = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m);
+  const float c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - m);
+  m_run = m;
+  l_run = l_run * c0 + l1 * c1;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_v p = *reinterpret_cast<const f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][4 * g + e] = o[i][4 * g + e] * c0 + p[e] * c1;
+    }
   if (!real) return;
   const int64_t to = ((int64_t)rb * a.n_heads + rh) * a.splits + split;
 #pragma unroll
@@ -467,28 +515,37 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   }
 }
 
-// Every token through workgroups of one sequence.
 template <int D, bool LOOP>
 __device__ __forceinline__ void attn_sequences(const CacheAttnArgs& a, float scale_log2, int i, char* smem) {
   const int per = a.n_kv_heads * a.own_splits, b = i / per, r = i - b * per;
-  attn_split<D, LOOP>(a, scale_log2, r / a.n_kv_heads, r % a.n_kv_heads, b, smem);
+  attn_split<D, 4, LOOP>(a, scale_log2, r / a.n_kv_heads, r % a.n_kv_heads, b, smem);
 }
+
+// Every token through workgroups of one sequence.
 template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void cache_attn_kernel(
     CacheAttnArgs a, float scale_log2) {
-  __shared__ __attribute__((aligned(16))) char smem[split_lds(D)];
+  __shared__ __attribute__((aligned(16))) char smem[split_lds(D, 4)];
   attn_sequences<D, false>(a, scale_log2, blockIdx.x, smem);
 }
+// One workgroup per (sequence, kv head), and no merge.
+template <int D, int NW, bool LOOP>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void cache_attn_direct_kernel(
+    CacheAttnArgs a, float scale_log2) {
+  __shared__ __attribute__((aligned(16))) char smem[split_lds(D, NW)];
+  attn_split<D, NW, LOOP, true>(a, scale_log2, 0, blockIdx.x % a.n_kv_heads, blockIdx.x / a.n_kv_heads, smem);
+}
+
 // The prefix's workgroups first (the longest), then the sequences'.
-template <int D, int RW>
+template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void cache_attn_shared_kernel(
     CacheAttnArgs a, float scale_log2) {
-  __shared__ __attribute__((aligned(1024))) char smem[prefix_lds(D, RW) > split_lds(D) ? prefix_lds(D, RW) : split_lds(D)];
-  const int tiles = (a.B * a.G + 32 * RW - 1) / (32 * RW);
+  __shared__ __attribute__((aligned(1024))) char smem[std::max(prefix_lds(D), split_lds(D, 4))];
+  const int tiles = (a.B * a.G + kTileRows - 1) / kTileRows;
   const int i = blockIdx.x, first = a.prefix_splits * tiles * a.n_kv_heads;
   if (i < first) {
     const int j = i / a.n_kv_heads;
-    return attn_prefix<D, RW>(a, scale_log2, j / tiles, j % tiles, i % a.n_kv_heads, smem);
+    return attn_prefix<D>(a, scale_log2, j / tiles, j % tiles, i % a.n_kv_heads, smem);
   }
   attn_sequences<D, true>(a, scale_log2, i - first, smem);
 }
@@ -559,12 +616,7 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int 
     if (t >= ctx) break;
     float p = 0.f;
     for (int gg = 0; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_m[gg]) * s_r[gg];
-    if (t == ctx - 1) {
-      if (a.pos) a.pos[row + t] = a.seen[b] - 1;
-    } else {
-      p += a.decay * a.acc[row + t];
-    }
-    a.acc_out[row + t] = p;
+    put_weight(a, row + t, b, t == ctx - 1, p);
   }
 }
 
@@ -580,30 +632,39 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
                               int64_t prefix_len, int64_t max_ctx, bool weights) {
   CacheAttnPlan p;
   const int64_t rows = B * (n_heads / n_kv_heads), blocks = (prefix_len + 15) / 16;
-  p.shared = B > 1 && prefix_len > 0 && blocks * 16 + max_ctx > kChunk;
-  p.row_groups = rows > 64 ? 4 : 2;
+  const int64_t slots = blocks * 16 + (max_ctx + 15) / 16 * 16;
+  // Alone: a step of 256 slots at least as fast as splits and their merge at any batch; longer
+  // ones where a workgroup per CU has enough of them (64 and more for 3 and 4 steps) and not
+  // too many. MI355X, in a graph, splits and merge -> alone: 3 sequences of 97 tokens, 4 heads
+  // 7.5 -> 3.4 us; 32 of 200, 8 kv heads 14.0 -> 6.1; 24 of 200, 40 heads 16.4 -> 14.3; 32 of 1000, 8 kv
+  // heads 25.4 -> 19.6. Left to the splits: 4 of 1000, 8 kv heads 9.2 (12.6 alone); 24 of 300 + 100,
+  // 40 heads 18.2 (28.3).
+  const int64_t groups = B * n_kv_heads;
+  p.direct = slots <= 256 || (groups <= 512 && slots <= (groups < 64 ? 512 : kDirect));
+  p.shared = !p.direct && B > 1 && prefix_len > 0;
   p.lead_blocks = p.shared ? 0 : (int)blocks;
-  p.own_chunks = 1;
+  p.own_blocks = p.direct ? kDirect / 16 : 8;
   p.prefix_tokens = 0;
   p.prefix_splits = 0;
   if (p.shared) {
     // Every split costs the batch a partial result (520 bytes per query head at D = 128, written
     // and read), so a split is as long as leaves 256 workgroups to the prefix, one per CU, and to
     // the sequences.
-    const int64_t tiles = (rows + 32 * p.row_groups - 1) / (32 * p.row_groups);
+    const int64_t tiles = (rows + kTileRows - 1) / kTileRows;
     p.prefix_tokens = (int)std::min<int64_t>(
         kPrefixBlocks * 16, std::max<int64_t>(128, (prefix_len * n_kv_heads * tiles / 256 + 63) / 64 * 64));
     p.prefix_splits = (prefix_len + p.prefix_tokens - 1) / p.prefix_tokens;
-    p.own_chunks = (int)std::min<int64_t>(4, std::max<int64_t>(1, B * n_kv_heads * ((max_ctx + kChunk - 1) / kChunk) / 256));
+    p.own_blocks = 8 * (int)std::min<int64_t>(4, std::max<int64_t>(1, B * n_kv_heads * ((max_ctx + 127) / 128) / 256));
   }
-  p.own_splits = (p.lead_blocks * 16ll + max_ctx + p.own_chunks * kChunk - 1) / (p.own_chunks * kChunk);
-  if (!p.shared) p.own_splits = std::max<int64_t>(1, p.own_splits);
+  p.own_splits = (p.lead_blocks + (max_ctx + 15) / 16 + p.own_blocks - 1) / p.own_blocks;
+  if (p.direct) p.own_splits = 1;
   p.splits = p.prefix_splits + p.own_splits;
   p.score_stride = weights ? (max_ctx + 15) / 16 * 16 : 0;
+  const int64_t parts = p.direct ? 0 : B * n_heads * p.splits;
   p.part_o = 0;
-  p.part_ml = p.part_o + B * n_heads * p.splits * D;
-  p.scores = (p.part_ml + B * n_heads * p.splits * 2 + 3) / 4 * 4;
-  p.floats = p.scores + B * n_heads * p.score_stride;
+  p.part_ml = parts * D;
+  p.scores = (p.part_ml + parts * 2 + 3) / 4 * 4;
+  p.floats = std::max<int64_t>(4, p.scores + B * n_heads * p.score_stride);
   return p;
 }
 
@@ -613,14 +674,14 @@ hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStr
       (a.ldq % 8) || a.B > 65535 || p.splits < 1)
     return hipErrorInvalidValue;
   const int chunks = a.acc_out ? (a.max_ctx + 1023) / 1024 : 0;
-  const int64_t tiles = ((int64_t)a.B * a.G + 32 * p.row_groups - 1) / (32 * p.row_groups);
+  const int64_t tiles = ((int64_t)a.B * a.G + kTileRows - 1) / kTileRows;
   const int64_t gx = (p.prefix_splits * tiles + a.B * p.own_splits) * a.n_kv_heads;
   const int64_t gm = a.n_heads + (int64_t)chunks * a.n_kv_heads;
   if (gx >= (1ll << 31) || gm >= (1ll << 31)) return hipErrorInvalidValue;
   a.lead_blocks = p.lead_blocks;
   a.prefix_tokens = p.prefix_tokens;
   a.prefix_splits = (int)p.prefix_splits;
-  a.own_chunks = p.own_chunks;
+  a.own_blocks = p.own_blocks;
   a.own_splits = (int)p.own_splits;
   a.splits = (int)p.splits;
   a.part_o = ws + p.part_o;
@@ -631,12 +692,17 @@ hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStr
   const dim3 grid((unsigned)gx), merge((unsigned)gm, a.B);
   const auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;
+    if (p.direct) {
+      const int slots = a.lead_blocks * 16 + (a.max_ctx + 15) / 16 * 16;
+      if (slots <= 128) hipLaunchKernelGGL((cache_attn_direct_kernel<D, 4, false>), grid, dim3(256), 0, s, a, sl);
+      else if (slots <= 256) hipLaunchKernelGGL((cache_attn_direct_kernel<D, 8, false>), grid, dim3(512), 0, s, a, sl);
+      else hipLaunchKernelGGL((cache_attn_direct_kernel<D, 8, true>), grid, dim3(512), 0, s, a, sl);
+      return;
+    }
     if (!p.shared)
       hipLaunchKernelGGL(cache_attn_kernel<D>, grid, dim3(256), 0, s, a, sl);
-    else if (p.row_groups == 4)
-      hipLaunchKernelGGL((cache_attn_shared_kernel<D, 4>), grid, dim3(256), 0, s, a, sl);
     else
-      hipLaunchKernelGGL((cache_attn_shared_kernel<D, 2>), grid, dim3(256), 0, s, a, sl);
+      hipLaunchKernelGGL(cache_attn_shared_kernel<D>, grid, dim3(256), 0, s, a, sl);
     hipLaunchKernelGGL(cache_attn_merge_kernel<D>, merge, dim3(256), 0, s, a);
   };
   if (a.D == 128) launch(std::integral_constant<int, 128>{});

@@ -279,7 +279,8 @@ def run_shared(c, dv=None, ldq=None, ldo=None, stream=None, ws=None):
 SHARED = [
     ([5], 0, 4, 4, 64), ([0], 1, 4, 4, 64), ([1, 0, 20], 77, 4, 4, 64), ([0, 0], 0, 8, 2, 128), ([0, 3], 0, 8, 8, 64),
     ([17, 128, 129, 0, 1], 16, 32, 8, 128), ([100, 5], 640, 32, 32, 128), ([300, 0, 16, 127], 129, 8, 4, 128),
-    ([33] * 9, 200, 16, 1, 128), ([2, 31], 500, 12, 1, 128), ([40, 7, 64], 333, 6, 2, 64), ([3] * 40, 300, 8, 2, 64),
+    ([33] * 9, 200, 16, 1, 128), ([2, 31], 500, 12, 1, 128), ([40, 7, 64], 333, 6, 2, 64), ([600, 1, 300], 1111, 6, 2, 64), ([200] * 19, 1040, 14, 2, 128),
+    ([1025], 0, 32, 8, 128), ([1024], 0, 4, 4, 64), ([513, 300], 0, 8, 2, 128), ([3] * 40, 300, 8, 2, 64),
     ([0] * 5, 1000, 10, 2, 128), ([700, 1300, 60], 15, 8, 8, 128), ([1, 2, 3] * 11, 513, 20, 4, 128), ([1] * 130, 90, 4, 1, 64),
     ([5] * 33, 2100, 16, 4, 64), ([64] * 70, 700, 8, 2, 128), ([9, 0, 30], 4100, 4, 4, 128)]
 
@@ -331,7 +332,8 @@ def test_attn_decode_shared_strides_and_lengths_outside():
 
 def test_attn_decode_shared_blocks_outside_the_pool():
     """A table entry that names no block of the pool: its tokens count as not cached."""
-    for lens, prefix, nh, nkv in (([40, 200], 70, 8, 2), ([40, 30] * 12, 300, 8, 2), ([10, 70], 300, 4, 4)):
+    for lens, prefix, nh, nkv in (([40, 200], 70, 8, 2), ([40, 30] * 12, 300, 8, 2), ([10, 70], 300, 4, 4), ([40, 30] * 20, 1300, 8, 2),
+                                  ([10, 700], 1300, 4, 4), ([1300, 1200], 50, 4, 2)):
         c = Cache(lens, prefix, nh, nkv, 128, 5)
         c.table[1, 1] = c.blocks
         c.prefix[2] = -1
@@ -341,12 +343,13 @@ def test_attn_decode_shared_blocks_outside_the_pool():
             assert np.all(np.abs(got[b] - o) <= tol), (lens, b)
 
 
+@pytest.mark.parametrize("prefix", [140, 1500])
 @pytest.mark.parametrize("what", [np.nan, np.inf])
-def test_attn_decode_shared_non_finite_stays_where_it_is(what):
+def test_attn_decode_shared_non_finite_stays_where_it_is(what, prefix):
     """A NaN or infinite value of one own token reaches its sequence and kv head alone; one in the
     prefix reaches every sequence, that kv head alone."""
     for prefix_token in (False, True):
-        c = Cache([40] * 10, 140, 8, 2, 128, 8)
+        c = Cache([40] * 10, prefix, 8, 2, 128, 8)
         if prefix_token:
             c.pool[c.prefix[3], 1, 1, 5] = what
         else:
@@ -361,11 +364,12 @@ def test_attn_decode_shared_non_finite_stays_where_it_is(what):
 
 def test_attn_decode_shared_large_scores():
     """Scores of several hundred, largest first, last and in the prefix: no overflow."""
-    c = Cache([70, 3, 0, 150], 200, 8, 4, 64, 21, std=9.0)
-    got = run_shared(c)
-    for b in range(4):
-        o, tol, _, _ = c.exact(b)
-        assert np.all(np.abs(got[b] - o) <= tol), b
+    for prefix in (200, 1400):
+        c = Cache([70, 3, 0, 150], prefix, 8, 4, 64, 21, std=9.0)
+        got = run_shared(c)
+        for b in range(4):
+            o, tol, _, _ = c.exact(b)
+            assert np.all(np.abs(got[b] - o) <= tol), (prefix, b)
 
 
 @pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED[:3] + SHARED[4:14] + [([2000, 1025, 1024], 0, 8, 2, 128), ([1500, 3], 100, 4, 4, 64)])
