@@ -141,6 +141,7 @@ hs_status cache_attn_call(CacheAttnArgs a, bool weights, void* ws, uint64_t ws_b
       (a.max_ctx && !a.block_table))
     return fail(HS_EINVAL, "bad arguments");
   a.G = a.n_heads / a.n_kv_heads;
+  if (!a.max_ctx) a.max_blocks = 0;  // no table to read
   if (a.max_ctx && a.max_blocks < (a.max_ctx + 15) / 16) return fail(HS_EINVAL, "block table too narrow");
   if (a.ldq < (int64_t)a.n_heads * a.D || a.ldo < (int64_t)a.n_heads * a.D)
     return fail(HS_EINVAL, "rows narrower than their heads");

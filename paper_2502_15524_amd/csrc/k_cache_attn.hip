@@ -26,25 +26,19 @@ namespace {
 constexpr int kDirect = 1024;  // slots that one workgroup takes alone at most
 typedef short s16x4_v __attribute__((ext_vector_type(4)));
 
-// The block that holds slots 16 j .. 16 j + 15 of sequence b, and how many
-// of them are tokens. Entries that name no block of the pool hold no tokens.
+// The block that holds slots 16 j .. 16 j + 15 of sequence b: its table entry (which does not
+// wait for the sequence's length; past the table: the last one), and how many of the slots
+// are tokens. Entries that name no block of the pool hold none.
 struct Block {
   int at, n;
 };
-__device__ __forceinline__ Block block_of(const CacheAttnArgs& a, int b, int j, int ctx) {
-  Block r{-1, 0};
-  if (j < a.lead_blocks) {
-    r.at = a.prefix[j];
-    r.n = min(16, a.prefix_len - 16 * j);
-  } else {
-    const int o = j - a.lead_blocks;
-    if (16 * o < ctx) {
-      r.at = a.block_table[(int64_t)b * a.max_blocks + o];
-      r.n = min(16, ctx - 16 * o);
-    }
-  }
-  if (r.at < 0 || r.at >= a.pool_blocks) r = Block{0, 0};
-  return r;
+__device__ __forceinline__ int entry_of(const CacheAttnArgs& a, int b, int j) {
+  if (j < a.lead_blocks) return a.prefix[j];
+  return a.max_blocks > 0 ? a.block_table[(int64_t)b * a.max_blocks + min(j - a.lead_blocks, a.max_blocks - 1)] : -1;
+}
+__device__ __forceinline__ Block block_of(const CacheAttnArgs& a, int entry, int j, int ctx) {
+  const int n = j < a.lead_blocks ? a.prefix_len - 16 * j : ctx - 16 * (j - a.lead_blocks);
+  return entry < 0 || entry >= a.pool_blocks || n <= 0 ? Block{0, 0} : Block{entry, min(16, n)};
 }
 
 // A buffer descriptor of uniform values, kept in scalar registers.
@@ -120,20 +114,23 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
   const auto s_acc = [&](int w) { return reinterpret_cast<float*>(sV(w)); };
   float(*const s_ml)[16][2] = reinterpret_cast<float(*)[16][2]>(smem + NW * 32 * LV * 2);
   float* const s_fin = reinterpret_cast<float*>(s_ml + NW);  // [16][2]
-  const int G = a.G, ctx = ctx_of(a, b), to = a.prefix_splits + split;
-  if (!DIRECT && to > 0 && to >= splits_of(a, ctx)) return;  // uniform across the workgroup
+  const int G = a.G, to = a.prefix_splits + split;
   const int tid = threadIdx.x, lane = tid & 63;
+  const int j0 = split * a.own_blocks;  // the split's first block
+  const int entry = entry_of(a, b, j0 + lane);
+  const int ctx = ctx_of(a, b);
+  asm volatile("" ::"v"(entry));  // not sunk below the branch
+  if (!DIRECT && to > 0 && to >= splits_of(a, ctx)) return;  // uniform across the workgroup
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 15, g = lane >> 4;
   const int64_t head_stride = (int64_t)16 * D, kv_stride = a.n_kv_heads * head_stride;
   const bf16_t* qrow = a.q + (int64_t)b * a.ldq + (int64_t)kh * G * D;
   const int crow = lane / CH, cch = lane % CH;
-  const int j0 = split * a.own_blocks;  // the split's first block
   const int left = a.lead_blocks + (ctx + 15) / 16 - j0;
   const int chunks = LOOP ? (min(a.own_blocks, left) + CB - 1) / CB : 1;
 
   // lane i holds the split's block i (at most 64)
-  const Block mine = block_of(a, b, j0 + lane, ctx);
+  const Block mine = block_of(a, entry, j0 + lane, ctx);
   Block blk[2];
   pack8 ck[2][NL], cv[2][NL];
   const auto load = [&](int c) {
@@ -594,13 +591,22 @@ __device__ __forceinline__ void merge_out(const CacheAttnArgs& a, int h, int b) 
   out[1] = pack2bf(o[2] * r, o[3] * r);
 }
 
-// What a sequence's own tokens received: 1024 tokens of one kv head.
+// What a sequence's own tokens received: 1024 tokens of one kv head, four to a thread. The
+// scores of the first four query heads and the old weights are requested with the splits'
+// statistics (past the sequence's tokens they may be anything).
 __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int b, int chunk) {
   __shared__ float s_m[16], s_r[16];
   const int ctx = ctx_of(a, b), n = splits_of(a, ctx), G = a.G;
-  const int t0 = chunk * 1024;
-  if (t0 >= ctx) return;  // uniform
+  const int t0 = chunk * 1024 + threadIdx.x;
+  if (chunk * 1024 >= ctx) return;  // uniform
   const int wave = threadIdx.x >> 6;
+  const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
+  const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
+  float x[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int gg = 0; gg < 4; ++gg) x[gg][i] = sc[min(gg, G - 1) * a.score_stride + min(t0 + i * 256, ctx - 1)];
   for (int gg = wave; gg < G; gg += 4) {
     float M, L;
     merge_ml(a.part_ml + ((int64_t)b * a.n_heads + kh * G + gg) * a.splits * 2, n, M, L);
@@ -608,14 +614,15 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int 
     s_r[gg] = L == 0.f ? 0.f : 1.f / L;
   }
   __syncthreads();
-  const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
-  const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int t = t0 + i * 256 + threadIdx.x;
+    const int t = t0 + i * 256;
     if (t >= ctx) break;
     float p = 0.f;
-    for (int gg = 0; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_m[gg]) * s_r[gg];
+#pragma unroll
+    for (int gg = 0; gg < 4; ++gg)
+      if (gg < G) p += fast_exp2(x[gg][i] - s_m[gg]) * s_r[gg];
+    for (int gg = 4; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_m[gg]) * s_r[gg];
     put_weight(a, row + t, b, t == ctx - 1, p);
   }
 }

@@ -23,7 +23,6 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kCopies = 8;        // of the first pass's histogram, by lane: most weights share a few exponents
 constexpr int kMovesHere = 256;   // per row at most, in the selecting workgroup
-constexpr int kHoles = 4096;      // listed in LDS
 constexpr int kMovesPerGroup = 32;
 
 // Larger keys stay. A NaN is below every weight, a protected token above all.
@@ -34,25 +33,6 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int64
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sums of the waves' totals before this wave, and of all.
-__device__ __forceinline__ uint32_t waves_before(const uint32_t* s_wave, int wave, uint32_t* all) {
-  uint32_t before = 0, sum = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; i += 4) {
-    const uint4 v = *reinterpret_cast<const uint4*>(s_wave + i);
-    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      before += i + j < wave ? x[j] : 0;
-      sum += x[j];
-    }
-  }
-  *all = sum;
-  return before;
-}
-__device__ __forceinline__ int rank_in(uint64_t ballot) {  // set lanes below this one
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0));
-}
 // Inclusive sum over the lanes up to this one.
 __device__ __forceinline__ uint32_t lane_scan(uint32_t v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
@@ -64,6 +44,15 @@ __device__ __forceinline__ uint32_t lane_scan(uint32_t v) {
   return v;
 }
 
+// Sums of the waves' totals (s_wave[0 .. 15]) before this wave, and of all.
+__device__ __forceinline__ uint32_t waves_before(const uint32_t* s_wave, int wave, uint32_t* all) {
+  const uint32_t v = s_wave[threadIdx.x & (kWaves - 1)], sum = lane_scan(v);  // (the first row of lanes)
+  *all = __builtin_amdgcn_readlane(sum, kWaves - 1);
+  return __builtin_amdgcn_readlane(sum - v, wave);
+}
+__device__ __forceinline__ int rank_in(uint64_t ballot) {  // set lanes below this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0));
+}
 // 16 bytes of a token in slot (block * 16 + offset) of the pool: chunk c of its key (c < D / 8)
 // or value
 template <int D>
@@ -72,24 +61,28 @@ __device__ __forceinline__ bf16_t* chunk_of(const KvEvictArgs& a, int slot, int 
   return a.pool + (((int64_t)(slot >> 4) * 2 + c / CH) * a.n_kv_heads + kh) * 16 * D + (slot & 15) * D + c % CH * 8;
 }
 
-// Moves [j0, j1) of a row, four chunks to a thread loaded before the first is stored.
-template <int D, int THREADS>
-__device__ __forceinline__ void move_tokens(const KvEvictArgs& a, const int2* pairs, int j0, int j1, int kh) {
+// Moves [j0, j1) of a row, four chunks to a thread loaded before the first is stored; pair(j):
+// from and to which slot of the pool (-1: left out).
+template <int D, int THREADS, typename F>
+__device__ __forceinline__ void move_tokens(const KvEvictArgs& a, F pair, int j0, int j1, int kh) {
   constexpr int CH = D / 4, U = 4;  // 16-byte chunks of a token
+  const int c = threadIdx.x % CH;
+  static_assert(THREADS % CH == 0, "a thread's chunks are alike");
   for (int i0 = j0 * CH; i0 < j1 * CH; i0 += U * THREADS) {
     pack8 v[U];
     int2 p[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * THREADS + threadIdx.x;
-      p[u] = i < j1 * CH ? pairs[i / CH] : make_int2(-1, -1);
+      p[u] = i < j1 * CH ? pair(i / CH) : make_int2(-1, -1);
+      if (p[u].y < 0) p[u].x = -1;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p[u].x >= 0) v[u] = ld16_nt(chunk_of<D>(a, p[u].x, kh, (i0 + u * THREADS + threadIdx.x) % CH));
+      if (p[u].x >= 0) v[u] = ld16_nt(chunk_of<D>(a, p[u].x, kh, c));
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p[u].x >= 0) st16(chunk_of<D>(a, p[u].y, kh, (i0 + u * THREADS + threadIdx.x) % CH), v[u]);
+      if (p[u].x >= 0) st16(chunk_of<D>(a, p[u].y, kh, c), v[u]);
   }
 }
 }  // namespace
@@ -101,11 +94,11 @@ __device__ __forceinline__ void move_tokens(const KvEvictArgs& a, const int2* pa
 template <int D, int K, bool MOVE>
 __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a) {
   constexpr int R = K > 0 ? K : 1;
-  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * kCopies + 3 * 256];
+  constexpr int kMoves = MOVE ? kMovesHere : 4096;  // listed in LDS
+  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * (kCopies + 3)];
   __shared__ __attribute__((aligned(16))) uint32_t s_wave[3][kWaves];
   __shared__ uint32_t s_pick[4][3];
-  __shared__ int s_table[R * 64], s_hole[kHoles];
-  __shared__ int2 s_pair[MOVE ? kMovesHere : 1];
+  __shared__ int s_table[R * 64], s_hole[kMoves], s_mover[kMoves];
   const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = (int64_t)b * a.n_kv_heads + kh;
@@ -128,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   }
   const int n = min(max(a.ctx[b], 0), a.max_ctx), kept = min(n, a.keep);
   const int64_t recent_from = (int64_t)a.seen[b] - a.recent;
-  for (int i = tid; i < 256 * kCopies + 3 * 256; i += kThreads) s_hist[i] = 0;
+  if (tid < 64 * (kCopies + 3)) *reinterpret_cast<uint4*>(s_hist + 4 * tid) = make_uint4(0, 0, 0, 0);
   if (kh == 0 && tid == 0) a.ctx_out[b] = kept;
   if constexpr (K == 0) per = (n + kThreads - 1) / kThreads;
   const int first = wave * 64 * per + lane;
@@ -165,9 +158,9 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   // the keep-th largest key, and how many of the tokens with that key stay
   uint32_t prefix = 0, mask = 0, need = a.keep;
   __syncthreads();
-#pragma unroll
-  for (int pass = 0; pass < 4; ++pass) {
-    const int shift = 24 - 8 * pass, copies = pass ? 1 : kCopies;
+  const auto select = [&](int pass, auto copies_) {
+    constexpr int copies = decltype(copies_)::value;
+    const int shift = 24 - 8 * pass;
     uint32_t* const hist = s_hist + (pass ? 256 * (kCopies + pass - 1) : 0);
     each([&](int t, float, int, uint32_t k) {
       if (t < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & 255) * copies + (lane & (copies - 1))], 1u);
@@ -175,7 +168,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     __syncthreads();
     if (wave == 0) {  // lane l has bins 255 - 4 l down to 252 - 4 l
       uint32_t c[4], sum = 0;
-      if (pass) {
+      if constexpr (copies == 1) {
         const uint4 v = *reinterpret_cast<const uint4*>(hist + 252 - 4 * lane);
         c[0] = v.w, c[1] = v.z, c[2] = v.y, c[3] = v.x;
       } else {
@@ -183,8 +176,8 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
         for (int j = 0; j < 4; ++j) {
           c[j] = 0;
 #pragma unroll
-          for (int i = 0; i < kCopies; i += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(hist + (255 - 4 * lane - j) * kCopies + i);
+          for (int i = 0; i < copies; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(hist + (255 - 4 * lane - j) * copies + i);
             c[j] += v.x + v.y + v.z + v.w;
           }
         }
@@ -209,7 +202,10 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     prefix |= s_pick[pass][0] << shift;
     mask |= 255u << shift;
     need = s_pick[pass][1];
-  }
+  };
+  select(0, std::integral_constant<int, kCopies>{});
+#pragma unroll 1  // (code that runs once comes from memory)
+  for (int pass = 1; pass < 4; ++pass) select(pass, std::integral_constant<int, 1>{});
 
   // the first `need` of the tokens with that key in slot order stay
   uint32_t all, eq = 0;
@@ -243,22 +239,36 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   holes = waves_before(s_wave[1], wave, &all);
   movers = waves_before(s_wave[2], wave, &all);
   const int moves = min((int)all, a.cap);
-  int2* const pairs = MOVE ? s_pair : reinterpret_cast<int2*>(a.lists) + row * a.cap;
-  const bool in_lds = a.cap <= kHoles;
+  int2* const pairs = reinterpret_cast<int2*>(a.lists) + row * a.cap;
+  const bool in_lds = a.cap <= kMoves;
   eq = eq0;
-  // the holes' list, and the weights of what keeps its slot
+  // the holes, the tokens that fill them, and the weights of what keeps its slot
   each([&](int t, float w, int p, uint32_t k) {
-    const bool s = stays(k, t), hole = t < a.keep && !s;
-    const uint64_t m = __ballot(hole);
-    const uint32_t j = holes + rank_in(m);
-    if (hole && j < (uint32_t)moves) {
-      if (in_lds) s_hole[j] = t;
-      else pairs[j].y = t;
+    const bool s = stays(k, t);
+    const int t_first = __builtin_amdgcn_readfirstlane(t);
+    if (t_first < a.keep) {
+      const bool hole = t < a.keep && !s;
+      const uint64_t m = __ballot(hole);
+      const uint32_t j = holes + rank_in(m);
+      if (hole && j < (uint32_t)moves) {
+        if (in_lds) s_hole[j] = t;
+        else pairs[j].y = t;
+      }
+      holes += __popcll(m);
+      if (t < a.keep && s) {
+        if (acc_out != acc) acc_out[t] = w;
+        if (pos_out != pos) pos_out[t] = p;
+      }
     }
-    holes += __popcll(m);
-    if (t < a.keep && s) {
-      if (acc_out != acc) acc_out[t] = w;
-      if (pos_out != pos) pos_out[t] = p;
+    if (t_first + 63 >= a.keep) {
+      const bool mover = t >= a.keep && s;
+      const uint64_t m = __ballot(mover);
+      const uint32_t j = movers + rank_in(m);
+      if (mover && j < (uint32_t)moves) {
+        if (in_lds) s_mover[j] = t;
+        else pairs[j].x = t;
+      }
+      movers += __popcll(m);
     }
   });
   __syncthreads();
@@ -266,40 +276,15 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     const int p = K > 0 ? s_table[t >> 4] : table[t >> 4];
     return p < 0 || p >= a.pool_blocks ? -1 : p * 16 + (t & 15);
   };
-  const auto put = [&](int j, int from, int to, float w, int p) {
-    const int x = slot_of(from), y = slot_of(to);
-    acc_out[to] = w;
-    pos_out[to] = p;
-    pairs[j] = x < 0 || y < 0 ? make_int2(-1, -1) : make_int2(x, y);
-  };
-  eq = eq0;
-  each([&](int t, float w, int p, uint32_t k) {
-    const bool mover = stays(k, t) && t >= a.keep;
-    const uint64_t m = __ballot(mover);
-    const uint32_t j = movers + rank_in(m);
-    if (mover && j < (uint32_t)moves) {
-      const int to = in_lds ? s_hole[j] : pairs[j].y;
-      if constexpr (K > 0) {
-        put(j, t, to, w, p);
-      } else {  // other waves may still read the row: in place, nothing of it is written yet
-        pairs[j] = make_int2(t, to);
-      }
-    }
-    movers += __popcll(m);
-  });
-  if constexpr (K == 0) {
-    __syncthreads();
-    for (int j = tid; j < moves; j += kThreads) {
-      const int2 m = pairs[j];
-      put(j, m.x, m.y, acc[m.x], pos[m.x]);
-    }
+  if constexpr (MOVE)
+    move_tokens<D, kThreads>(a, [&](int j) { return make_int2(slot_of(s_mover[j]), slot_of(s_hole[j])); }, 0, moves, kh);
+  for (int j = tid; j < moves; j += kThreads) {
+    const int from = in_lds ? s_mover[j] : pairs[j].x, to = in_lds ? s_hole[j] : pairs[j].y;
+    acc_out[to] = acc[from];
+    pos_out[to] = pos[from];
+    if constexpr (!MOVE) pairs[j] = make_int2(slot_of(from), slot_of(to));
   }
-  if constexpr (MOVE) {
-    __syncthreads();
-    move_tokens<D, kThreads>(a, s_pair, 0, moves, kh);
-  } else {
-    if (tid == 0) a.counts[row] = moves;
-  }
+  if (!MOVE && tid == 0) a.counts[row] = moves;
 }
 
 template <int D>
@@ -308,7 +293,8 @@ __global__ __launch_bounds__(256) void kv_evict_move_kernel(KvEvictArgs a) {
   const int64_t row = (int64_t)blockIdx.z * a.n_kv_heads + kh;
   const int moves = a.counts[row];
   if (j0 >= moves) return;
-  move_tokens<D, 256>(a, reinterpret_cast<const int2*>(a.lists) + row * a.cap, j0, min(j0 + kMovesPerGroup, moves), kh);
+  const int2* pairs = reinterpret_cast<const int2*>(a.lists) + row * a.cap;
+  move_tokens<D, 256>(a, [&](int j) { return pairs[j]; }, j0, min(j0 + kMovesPerGroup, moves), kh);
 }
 
 hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
