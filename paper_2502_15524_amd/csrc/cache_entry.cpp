@@ -38,8 +38,8 @@ hs_status ws_ok(const void* ws, uint64_t bytes, uint64_t need) {
   return HS_OK;
 }
 
-// Angle per position of every pair, in turns.
-hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, double* turns) {
+// Angle per position of every pair, in units of 2^-64 turns (whole turns do not count).
+hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, uint64_t* turns) {
   constexpr double kTwoPi = 6.283185307179586476925;
   if (c.kind < HS_ROPE_PLAIN || c.kind > HS_ROPE_YARN) return fail(HS_EINVAL, "unknown rotary scaling");
   if (!(c.magnitude > 0) || !std::isfinite(c.magnitude)) return fail(HS_EINVAL, "magnitude must be positive");
@@ -60,7 +60,8 @@ hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, double*
     if (c.kind == HS_ROPE_YARN) keep = 1.0 - (i - a) / std::max(b - a, 1e-3);
     keep = std::min(1.0, std::max(0.0, keep));
     if (keep < 1.0) w = (1.0 - keep) * w / c.factor + keep * w;
-    turns[i] = w / kTwoPi;
+    const double t = w / kTwoPi;
+    turns[i] = static_cast<uint64_t>(ldexp(t - floor(t), 64));
   }
   return HS_OK;
 }
@@ -75,7 +76,7 @@ extern "C" hs_status hs_k_rope_tables(float* cos_t, float* sin_t, int32_t max_po
     if (!aligned(cos_t, 16) || !aligned(sin_t, 16)) return fail(HS_EINVAL, "tables not 16-byte aligned");
     const hs_rope_scaling plain{HS_ROPE_PLAIN, 0, 1.0, 0.0, 0.0, 1.0};
     const hs_rope_scaling& c = scaling ? *scaling : plain;
-    double turns[64];
+    uint64_t turns[64];
     const hs_status r = rope_turns(rot_dim, base, c, turns);
     if (r != HS_OK) return r;
     return done(rope_tables(cos_t, sin_t, max_pos, rot_dim / 2, turns, (float)c.magnitude,

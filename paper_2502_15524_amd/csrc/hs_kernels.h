@@ -152,8 +152,8 @@ hipError_t meta_pull(const int32_t* host, int32_t* dev, int64_t n, hipStream_t s
 hipError_t kv_copy(const uint64_t* src, const uint64_t* dst, const int32_t* valid, int n_units,
                    int64_t unit_bytes, int D, int zero_tail, hipStream_t s, LaunchInfo* info);
 
-// cos and sin of 2 pi p turns[i], times magnitude: [max_pos][half] each.
-hipError_t rope_tables(float* cos_t, float* sin_t, int max_pos, int half, const double* turns,
+// cos and sin of 2 pi p turns[i] (in units of 2^-64), times magnitude: [max_pos][half] each.
+hipError_t rope_tables(float* cos_t, float* sin_t, int max_pos, int half, const uint64_t* turns,
                        float magnitude, hipStream_t s);
 
 // Rotation of the first `rot` elements of every query and key head at given
