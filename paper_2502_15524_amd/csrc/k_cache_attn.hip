@@ -55,16 +55,22 @@ __device__ __forceinline__ pack8 ld16_once(__amdgpu_buffer_rsrc_t r, int off) {
   return __builtin_bit_cast(pack8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kNonTemporal));
 }
 
-// Merged statistics of a query head of a sequence: the splits' largest score
-// and the sum relative to it. Called by a whole wave; the order is fixed.
-__device__ __forceinline__ void merge_ml(const float* ml, int n, float& M, float& L) {
+// (largest score, sum) of the split that the lane has among the first 64, requested without
+// waiting for the sequence's length: past its splits it may be anything.
+__device__ __forceinline__ float2 first_ml(const CacheAttnArgs& a, const float* ml) {
+  const int s = min((int)(threadIdx.x & 63), a.splits - 1);
+  return make_float2(ml[2 * s], ml[2 * s + 1]);
+}
+// Merged statistics of a query head of a sequence of n splits: the largest score and the
+// sum relative to it. Called by a whole wave; the order is fixed.
+__device__ __forceinline__ void merge_ml(const float* ml, float2 first, int n, float& M, float& L) {
   const int lane = threadIdx.x & 63;
-  M = -INFINITY;
-  for (int s = lane; s < n; s += 64) M = fmaxf(M, ml[2 * s]);
+  M = lane < n ? first.x : -INFINITY;
+  for (int s = lane + 64; s < n; s += 64) M = fmaxf(M, ml[2 * s]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-  L = 0.f;
-  for (int s = lane; s < n; s += 64) {
+  L = lane < n && first.x != -INFINITY ? first.y * fast_exp2(first.x - M) : 0.f;
+  for (int s = lane + 64; s < n; s += 64) {
     const float m = ml[2 * s];
     if (m != -INFINITY) L += ml[2 * s + 1] * fast_exp2(m - M);
   }
@@ -334,14 +340,6 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   const int G = a.G, row = (tile * RW + rw) * 32 + q, rows = a.B * G;
   const bool real = row < rows;
   const int rb = row / G, rh = kh * G + row - rb * G;
-  bf16x8_v qf[D / 16];
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    qf[ks] = as_bf16x8(real ? ld16(a.q + (int64_t)rb * a.ldq + rh * D + ks * 16 + hi * 8) : zero8());
-  // (waited for here: left to their first use, in the loop, the wait would drain the copies)
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
-
   int ko[PER], vo[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -369,6 +367,10 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   };
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i) request(i);
+  bf16x8_v qf[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+    qf[ks] = as_bf16x8(real ? ld16(a.q + (int64_t)rb * a.ldq + rh * D + ks * 16 + hi * 8) : zero8());
 
   int ka[D / 16], va[D / 32][2];
 #pragma unroll
@@ -389,6 +391,11 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
   const bool busy = (tile * RW + rw) * 32 < rows;  // of the wave
+
+  // (the queries are waited for here, with the first step's copies: left to their first use, in
+  // the loop, the wait would drain the copies in flight)
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
 
   for (int k = 0; k < steps; ++k) {
     // this wave's copies of step k have landed (those of the NST - 2 steps after it may be
@@ -548,27 +555,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void c
 }
 
 // The output of one (query head, sequence). A row of 16-byte loads takes D / 4 lanes, so
-// the four waves take 4 * 256 / D splits at a time, up to 64 with all loads in flight (they
-// do not wait for the statistics; rows past the last split re-read it, with weight 0).
+// the four waves take 4 * 256 / D splits at a time, up to 64 with all loads in flight; those of
+// the first 64 do not wait for the sequence's length.
 template <int D>
 __device__ __forceinline__ void merge_out(const CacheAttnArgs& a, int h, int b) {
   constexpr int LPR = D / 4, RPP = 64 / LPR, U = 16 / RPP;  // lanes per row, rows per wave and load, loads
   __shared__ f32x4_v s_o[4][LPR];
-  const int ctx = ctx_of(a, b), n = splits_of(a, ctx);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = ((int64_t)b * a.n_heads + h) * a.splits;
   const float* ml = a.part_ml + row * 2;
-  f32x4_v o = {0.f, 0.f, 0.f, 0.f};
-  float M, L;
-  for (int s0 = 0; s0 < n; s0 += 64) {
-    f32x4_v v[U];
+  f32x4_v v[U], o = {0.f, 0.f, 0.f, 0.f};
+  const auto load = [&](int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int s = min(s0 + (4 * u + wave) * RPP + lane / LPR, n - 1);
-      v[u] = *reinterpret_cast<const f32x4_v*>(a.part_o + (row + s) * D + (lane % LPR) * 4);
+      const int s = min(s0 + (4 * u + wave) * RPP + lane / LPR, a.splits - 1);
+      if (s0 + (4 * u + wave) * RPP < a.splits)  // uniform
+        v[u] = *reinterpret_cast<const f32x4_v*>(a.part_o + (row + s) * D + (lane % LPR) * 4);
     }
-    const float m = s0 + lane < n ? ml[2 * (s0 + lane)] : -INFINITY;
-    if (s0 == 0) merge_ml(ml, n, M, L);
+  };
+  load(0);
+  const float2 first = first_ml(a, ml);
+  const int ctx = ctx_of(a, b), n = splits_of(a, ctx);
+  float M, L;
+  merge_ml(ml, first, n, M, L);
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    if (s0 > 0) load(s0);
+    const float m = s0 + lane >= n ? -INFINITY : s0 == 0 ? first.x : ml[2 * (s0 + lane)];
     const float w = m == -INFINITY ? 0.f : fast_exp2(m - M);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -596,20 +608,21 @@ __device__ __forceinline__ void merge_out(const CacheAttnArgs& a, int h, int b) 
 // statistics (past the sequence's tokens they may be anything).
 __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int b, int chunk) {
   __shared__ float s_m[16], s_r[16];
-  const int ctx = ctx_of(a, b), n = splits_of(a, ctx), G = a.G;
-  const int t0 = chunk * 1024 + threadIdx.x;
-  if (chunk * 1024 >= ctx) return;  // uniform
-  const int wave = threadIdx.x >> 6;
+  const int G = a.G, t0 = chunk * 1024 + threadIdx.x, wave = threadIdx.x >> 6;
   const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
   const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
   float x[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int gg = 0; gg < 4; ++gg) x[gg][i] = sc[min(gg, G - 1) * a.score_stride + min(t0 + i * 256, ctx - 1)];
+    for (int gg = 0; gg < 4; ++gg) x[gg][i] = sc[min(gg, G - 1) * a.score_stride + min(t0 + i * 256, a.max_ctx - 1)];
+  const float2 first = first_ml(a, a.part_ml + ((int64_t)b * a.n_heads + kh * G + min(wave, G - 1)) * a.splits * 2);
+  const int ctx = ctx_of(a, b), n = splits_of(a, ctx);
+  if (chunk * 1024 >= ctx) return;  // uniform
   for (int gg = wave; gg < G; gg += 4) {
     float M, L;
-    merge_ml(a.part_ml + ((int64_t)b * a.n_heads + kh * G + gg) * a.splits * 2, n, M, L);
+    const float* ml = a.part_ml + ((int64_t)b * a.n_heads + kh * G + gg) * a.splits * 2;
+    merge_ml(ml, gg == wave ? first : first_ml(a, ml), n, M, L);
     s_m[gg] = M == -INFINITY ? 0.f : M;
     s_r[gg] = L == 0.f ? 0.f : 1.f / L;
   }
@@ -661,7 +674,9 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
     p.prefix_tokens = (int)std::min<int64_t>(
         kPrefixBlocks * 16, std::max<int64_t>(128, (prefix_len * n_kv_heads * tiles / 256 + 63) / 64 * 64));
     p.prefix_splits = (prefix_len + p.prefix_tokens - 1) / p.prefix_tokens;
-    p.own_blocks = 8 * (int)std::min<int64_t>(4, std::max<int64_t>(1, B * n_kv_heads * ((max_ctx + 127) / 128) / 256));
+    // up to 512 of its slots in one split; longer ones in splits of 384 (of 256, 384, 512 and 1024 the
+    // best for ragged caches of 512 to 4096 tokens: 51.4, 49.0, 51.5 and 55.9 us for 24 of them)
+    p.own_blocks = 8 * (int)std::min<int64_t>(max_ctx > 512 ? 3 : 4, std::max<int64_t>(1, groups * ((max_ctx + 127) / 128) / 256));
   }
   p.own_splits = (p.lead_blocks + (max_ctx + 15) / 16 + p.own_blocks - 1) / p.own_blocks;
   if (p.direct) p.own_splits = 1;
