@@ -156,7 +156,8 @@ hs_status hs_k_attn_decode_noalloc(const void* q, int64_t ldq, const void* pool,
  * in `ws`, device memory of the caller, 16-byte aligned, of at least the bytes
  * that the matching _ws function gives (HS_ERANGE below it). ws need not be
  * cleared, and calls that may overlap in time need one each, replays of
- * captured calls too. Buffers and the stream belong to the current device. B is at
+ * captured calls too. Outputs overlap neither inputs nor each other but where it
+ * says so. Buffers and the stream belong to the current device. B is at
  * most 65535, prefix_len and max_ctx at most 2^30, pool_blocks 2^27.
  * Results are deterministic. */
 

@@ -30,6 +30,14 @@ hs_status heads_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
   return HS_OK;
 }
 
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uint64_t x = reinterpret_cast<uint64_t>(a), y = reinterpret_cast<uint64_t>(b);
+  return x < y + nb && y < x + na;
+}
+// Bytes from the first to the last element of rows of bf16.
+uint64_t rows_bytes(int64_t rows, int64_t ld, int64_t width) { return 2ull * ((rows - 1) * ld + width); }
+
 hs_status ws_ok(const void* ws, uint64_t bytes, uint64_t need) {
   if (bytes < need)
     return fail(HS_ERANGE, "workspace of " + std::to_string(bytes) + " bytes, needs " + std::to_string(need));
@@ -109,6 +117,14 @@ extern "C" hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t*
         !aligned(k_out, 16) || !aligned(pool, 16) || !aligned(cos_t, 16) || !aligned(sin_t, 16) ||
         !aligned(pos, 4) || !aligned(slot, 4))
       return fail(HS_EINVAL, "pointers or row strides not aligned");
+    // in place, or apart
+    const int64_t nq = (int64_t)n_heads * head_dim, nk = (int64_t)n_kv_heads * head_dim;
+    const uint64_t in = rows_bytes(T, ldqkv, nq + 2 * nk);
+    const void* const keys = static_cast<const bf16_t*>(qkv) + nq;
+    if (overlap(qkv, in, q_out, rows_bytes(T, ldq, nq)) && (q_out != qkv || ldq != ldqkv))
+      return fail(HS_EINVAL, "q_out overlaps qkv without being it");
+    if (k_out && overlap(qkv, in, k_out, rows_bytes(T, ldk, nk)) && (k_out != keys || ldk != ldqkv))
+      return fail(HS_EINVAL, "k_out overlaps qkv without being its keys");
     RopeKvAtArgs a{static_cast<const bf16_t*>(qkv), ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim,
                    layout == 1, static_cast<bf16_t*>(q_out), ldq, static_cast<bf16_t*>(k_out), k_out ? ldk : 0,
                    static_cast<bf16_t*>(pool), pool_blocks, T, n_heads, n_kv_heads, head_dim};
@@ -123,7 +139,12 @@ hs_status cache_attn_sizes(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32
                            int32_t prefix_len, int32_t max_ctx) {
   if (B < 1 || B > 65535 || prefix_len < 0 || max_ctx < 0 || prefix_len > 1 << 30 || max_ctx > 1 << 30)
     return fail(HS_EINVAL, "bad arguments");
-  return heads_ok(n_heads, n_kv_heads, head_dim);
+  const hs_status h = heads_ok(n_heads, n_kv_heads, head_dim);
+  if (h != HS_OK) return h;
+  // partial results and scores fit 2^50 bytes, so no size or index below overflows
+  if ((double)B * n_heads * ((prefix_len + (double)max_ctx) / 128 + 2) * (head_dim + 130) > (double)(1ll << 48))
+    return fail(HS_EINVAL, "too many sequences, heads and tokens");
+  return HS_OK;
 }
 
 hs_status cache_attn_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -232,6 +253,8 @@ namespace {
 hs_status evict_sizes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
   if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || keep < 1 || max_ctx < 1 || max_ctx > 1 << 30)
     return fail(HS_EINVAL, "bad arguments");
+  if ((double)B * n_kv_heads * max_ctx > (double)(1ll << 48))
+    return fail(HS_EINVAL, "too many sequences, heads and tokens");
   return HS_OK;
 }
 // moves a row can have

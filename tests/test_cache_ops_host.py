@@ -39,6 +39,24 @@ def test_rope_kv_refuses(change):
     refused(hs.HS_EINVAL, hs.hs_k_rope_kv, **a)
 
 
+@pytest.mark.parametrize("change", [
+    dict(q_out=P, ldq=48 * 128 + 8), dict(q_out=P + 256), dict(q_out=P - 4096), dict(k_out=P, ldk=48 * 128), dict(k_out=P + 32 * 256, ldk=1024),
+    dict(k_out=P + 33 * 256, ldk=48 * 128)])
+def test_rope_kv_refuses_rows_that_overlap(change):
+    a = dict(qkv=P, ldqkv=48 * 128, pos=P, slot=P, cos_t=P, sin_t=P, max_pos=64, rot_dim=128, layout="half", q_out=16 * P, ldq=32 * 128,
+             k_out=0, ldk=1024, pool=32 * P, pool_blocks=4, T=3, n_heads=32, n_kv_heads=8, head_dim=128) | change
+    refused(hs.HS_EINVAL, hs.hs_k_rope_kv, **a)
+
+
+def test_sizes_that_would_overflow_are_refused():
+    for fn in (hs.hs_k_attn_decode_shared_ws, hs.hs_k_attn_decode_weights_ws):
+        refused(hs.HS_EINVAL, fn, 65535, 65536, 65536, 128, 1 << 30, 1 << 30)
+        refused(hs.HS_EINVAL, fn, 1, 32, 8, 128, (1 << 30) + 1, 1)
+        assert fn(64, 32, 8, 128, 1 << 20, 1 << 20) > 0
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 65535, 65535, 1 << 29, 1 << 30)
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict, **(EVICT | dict(pool_blocks=(1 << 27) + 1)))
+
+
 ATTN = dict(q=P, ldq=4096, pool=P, pool_blocks=9, prefix=P, prefix_len=100, block_table=P, ctx=P, out=P, ldo=4096, B=2, n_heads=32,
             n_kv_heads=8, head_dim=128, max_blocks=4, max_ctx=64, ws=P, ws_bytes=1 << 40)
 WEIGHTS = ATTN | dict(acc=P, acc_out=P, acc_stride=64, decay=1.0, pos=P, seen=P)

@@ -528,6 +528,51 @@ def test_kv_evict_moves_outside_the_pool_are_left_out():
     assert np.array_equal(dpool.cpu().numpy().view(np.uint16), want)
 
 
+def test_blocks_past_four_gigabytes():
+    """The same cache at the start of a small pool and behind 4.3 GiB of a large one: attention, rotation
+    and append, and eviction give the same bits."""
+    torch = G.torch()
+    hs = _hs()
+    for lens, prefix in (([40, 7], 100), ([700, 900], 1500)):
+        c = Cache(lens, prefix, 32, 16, 128, 3, wild=False)
+        first = (4 << 30) // (2 * 16 * 16 * 128 * 2) + 2500
+        small = c.device()
+        big = torch.zeros((first + c.blocks,) + c.pool.shape[1:], dtype=torch.bfloat16, device="cuda")
+        big[first:] = small["pool"]
+        far = dict(small, pool=big, prefix=small["prefix"] + first, table=small["table"] + first)
+        a = run_shared(c, small)
+        near_blocks, c.blocks = c.blocks, first + c.blocks
+        b = run_shared(c, far)
+        assert np.array_equal(a, b)
+        n, keep = max(lens), 24
+        rng = np.random.default_rng(1)
+        ctx, seen = small["ctx"], dev(np.full(2, n, np.int32))
+        outs = []
+        for dv, blocks in ((small, near_blocks), (far, c.blocks)):
+            acc, pos = dev(np.exp(rng.standard_normal((2, 16, n))).astype(np.float32)), dev(np.zeros((2, 16, n), np.int32) + np.arange(n, dtype=np.int32))
+            if outs:
+                acc.copy_(first_acc)
+            first_acc = acc.clone()
+            qkv = dev_bf(bf(np.random.default_rng(2), (2, 64 * 128)))
+            q = torch.zeros((2, 32 * 128), dtype=torch.bfloat16, device="cuda")
+            slot = (dv["table"][:, 0] * 16 + 5).to(torch.int32).contiguous()
+            assert slot.max() < blocks * 16
+            at = dev(np.array([3, 8], np.int32))
+            cs = dev(np.cos(np.arange(10 * 64, dtype=np.float32)).reshape(10, 64))
+            hs.hs_k_rope_kv(qkv.data_ptr(), 64 * 128, at.data_ptr(), slot.data_ptr(), cs.data_ptr(), cs.data_ptr(), 10, 128, "half",
+                            q.data_ptr(), 32 * 128, 0, 0, dv["pool"].data_ptr(), blocks, 2, 32, 16, 128, G.stream_ptr())
+            nb = hs.hs_k_kv_evict_ws(2, 16, keep, n)
+            ws, left = workspace(nb), torch.zeros(2, dtype=torch.int32, device="cuda")
+            hs.hs_k_kv_evict(dv["pool"].data_ptr(), blocks, dv["table"].data_ptr(), ctx.data_ptr(), seen.data_ptr(), acc.data_ptr(),
+                             pos.data_ptr(), n, acc.data_ptr(), pos.data_ptr(), n, left.data_ptr(), keep, 0, 4, 2, 16, 128, c.width, n,
+                             ws.data_ptr(), nb, G.stream_ptr())
+            torch.cuda.synchronize()
+            outs.append([host(x) for x in (dv["pool"][-near_blocks:], acc, pos, q, left)])
+        for x, y in zip(*outs):
+            assert np.array_equal(x, y)
+        del big, far
+
+
 # ----------------------------------------------------------------- together
 
 class Budget:
