@@ -10,10 +10,16 @@
 // to bf16 for the second matrix product only (an error of half a bf16 step, as
 // the output's own rounding), their sum and the weights are of the unrounded ones.
 //
-// Two kinds of workgroup: of 128 slots of one (sequence, kv head), with the G query
-// heads of the kv head as the rows; and of many tokens of the prefix and one kv
-// head, with the G query heads of all sequences as the rows, so that the prefix is
-// read once for the batch.
+// Two kinds of workgroup: of one sequence and kv head, with the kv head's G query heads as the
+// rows; and of a part of the prefix and one kv head, with the G query heads of all
+// sequences as the rows, so that the prefix is read once for the batch. Short sequences
+// are one split, whose workgroup writes output and weights without a second kernel.
+//
+// Bound by HBM: every cached key and value is read once. MI355X, merge included: 8B heads, 32
+// sequences of 64 to 512 tokens behind 8192 22.3 us (72 MB: 3.2 TB/s; the prefix takes 19.5 us, of
+// which 3.7 are the first copies' way and 8 its eight steps, its partial results' merge 4); 13B
+// heads, 24 of up to 300 behind 2011 28.0 us (4.2 TB/s); with weights, 24 of 512 to 4096 behind 1000
+// 54.4 us (4.5 TB/s).
 #include "hs_device.h"
 #include "hs_kernels.h"
 
@@ -85,13 +91,9 @@ __device__ __forceinline__ int ctx_of(const CacheAttnArgs& a, int b) {
   return min(max(a.ctx[b], 0), a.max_ctx);
 }
 // What a token received, added to what it had; the newest starts with it, and gets its position.
-__device__ __forceinline__ void put_weight(const CacheAttnArgs& a, int64_t at, int b, bool newest, float p) {
-  if (newest) {
-    if (a.pos) a.pos[at] = a.seen[b] - 1;
-  } else {
-    p += a.decay * a.acc[at];
-  }
-  a.acc_out[at] = p;
+__device__ __forceinline__ void put_weight(const CacheAttnArgs& a, int64_t at, int b, bool newest, float old, float p) {
+  if (newest && a.pos) a.pos[at] = a.seen[b] - 1;
+  a.acc_out[at] = newest ? p : a.decay * old + p;
 }
 }  // namespace
 
@@ -102,11 +104,14 @@ __device__ __forceinline__ void put_weight(const CacheAttnArgs& a, int64_t at, i
 // V^T fragments come from transposing LDS reads. Keys and values are read in
 // whole rows, all of them requested before the first is used, and staged
 // through the wave's own LDS buffer, the keys first, then the values over them.
+//
+// NW waves, a step of 32 NW slots; LOOP: as many steps as the split has, the next one's rows
+// requested before this one's products, else one. DIRECT: the sequence is one split, and the
+// workgroup writes the output and the weights.
+
 // bytes of LDS: the waves' buffers and statistics, the merged statistics of the direct form
 constexpr int split_lds(int D, int NW) { return NW * 32 * (D + 16) * 2 + (NW + 1) * 16 * 2 * 4; }
 
-// NW waves, a step of 32 NW slots; LOOP: as many steps as the split has, else one. DIRECT: the
-// sequence is one split, and the workgroup writes the output and the weights.
 template <int D, int NW, bool LOOP, bool DIRECT = false>
 __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_log2, int split, int kh,
                                            int b, char* smem) {
@@ -285,9 +290,10 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
     const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
     const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
     for (int t = tid; t < ctx; t += 64 * NW) {
+      const float old = a.acc[row + t];
       float p = 0.f;
       for (int gg = 0; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_fin[2 * gg]) * s_fin[2 * gg + 1];
-      put_weight(a, row + t, b, t == ctx - 1, p);
+      put_weight(a, row + t, b, t == ctx - 1, old, p);
     }
   }
 }
@@ -611,7 +617,9 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int 
   const int G = a.G, t0 = chunk * 1024 + threadIdx.x, wave = threadIdx.x >> 6;
   const int64_t row = ((int64_t)b * a.n_kv_heads + kh) * a.acc_stride;
   const float* sc = a.scores + ((int64_t)b * a.n_heads + kh * G) * a.score_stride;
-  float x[4][4];
+  float x[4][4], old[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) old[i] = a.acc[row + min(t0 + i * 256, a.max_ctx - 1)];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -636,7 +644,7 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int kh, int 
     for (int gg = 0; gg < 4; ++gg)
       if (gg < G) p += fast_exp2(x[gg][i] - s_m[gg]) * s_r[gg];
     for (int gg = 4; gg < G; ++gg) p += fast_exp2(sc[gg * a.score_stride + t] - s_m[gg]) * s_r[gg];
-    put_weight(a, row + t, b, t == ctx - 1, p);
+    put_weight(a, row + t, b, t == ctx - 1, old[i], p);
   }
 }
 
