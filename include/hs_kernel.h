@@ -4,7 +4,8 @@
  * These run one of the engine's HIP kernels on caller-owned device buffers,
  * exactly as the stage forward pass launches it. They exist so that each
  * kernel can be checked against a reference and timed on its own; serving
- * goes through hs.h. All pointers are device pointers owned by the caller;
+ * goes through hs.h. The cache operators at the end are operators of their own, for
+ * servers that call the attention themselves. All pointers are device pointers owned by the caller;
  * `stream` is a hipStream_t (NULL = the null stream). Work is asynchronous,
  * except where an entry says that it waits.
  * Shapes the kernel does not support return HS_EINVAL before any launch.

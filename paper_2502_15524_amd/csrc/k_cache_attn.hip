@@ -725,7 +725,7 @@ hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStr
   const int64_t tiles = ((int64_t)a.B * a.G + kTileRows - 1) / kTileRows;
   const int64_t gx = (p.prefix_splits * tiles + a.B * p.own_splits) * a.n_kv_heads;
   const int64_t gm = a.n_heads + (int64_t)chunks * a.n_kv_heads;
-  if (gx >= (1ll << 31) || gm >= (1ll << 31)) return hipErrorInvalidValue;
+  if (gx >= (1ll << 23) || gm >= (1ll << 24)) return hipErrorInvalidValue;  // 2^32 threads of a launch
   a.lead_blocks = p.lead_blocks;
   a.prefix_tokens = p.prefix_tokens;
   a.prefix_splits = (int)p.prefix_splits;

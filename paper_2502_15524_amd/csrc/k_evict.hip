@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256) void kv_evict_move_kernel(KvEvictArgs a) {
 hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
   if (a.B <= 0) return hipSuccess;
   if ((a.D != 64 && a.D != 128) || a.n_kv_heads < 1 || a.n_kv_heads > 65535 || a.B > 65535 ||
-      a.keep < 1 || a.cap < 0)
+      a.keep < 1 || a.cap < 0 || a.cap >= 1 << 28)  // (2^32 threads of a launch)
     return hipErrorInvalidValue;
   const dim3 grid(a.n_kv_heads, a.B);
   // One launch for up to 512 moves a row, to 1024 where the rows fill the chip. MI355X, moved in the

@@ -74,7 +74,7 @@ hipError_t rope_tables(float* cos_t, float* sin_t, int max_pos, int half, const 
   RopeFreq f;
   for (int i = 0; i < 64; ++i) f.turns[i] = i < half ? turns[i] : 0;
   const int64_t n = ((int64_t)max_pos + 3) / 4 * (half / 4);
-  if ((n + 255) / 256 >= (1ll << 31)) return hipErrorInvalidValue;
+  if (n >= (1ll << 32) - 256) return hipErrorInvalidValue;  // threads of a launch
   hipLaunchKernelGGL(rope_tables_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, cos_t,
                      sin_t, max_pos, half, f, magnitude);
   return hipGetLastError();
@@ -158,7 +158,7 @@ hipError_t rope_kv_at(const RopeKvAtArgs& a, hipStream_t s) {
       (a.ldqkv % 8) || (a.ldq % 8) || (a.ldk % 8))
     return hipErrorInvalidValue;
   const int64_t per = (int64_t)(a.n_heads + 2 * a.n_kv_heads) * (a.D / 16), n = (a.T * per + 255) / 256;
-  if (per >= (1ll << 31) || n >= (1ll << 31)) return hipErrorInvalidValue;
+  if (per >= (1ll << 31) || n >= (1ll << 24)) return hipErrorInvalidValue;  // threads of a launch
   if (a.interleaved)
     hipLaunchKernelGGL(rope_kv_at_kernel<false>, dim3((unsigned)n), dim3(256), 0, s, a, (int)per);
   else
