@@ -330,7 +330,7 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
   constexpr int CH = D / 8, ROW = D * 2, BLK = KB * ROW, STG = 2 * BLK;
   constexpr int KPI = 64 / CH, PER = KB / KPI / 4;  // keys per copy; copies per wave, operand and step
   static_assert(PER >= 1 && PER * KPI * 4 == KB && 16 % (PER * KPI) == 0, "a wave's copies stay within a block");
-  static_assert(RW * 32 * D * 4 + RW * 256 <= NST * STG, "the token groups' merge fits the ring");
+  static_assert(RW * 32 * D * 4 + 4 * 32 * 8 <= NST * STG, "the token groups' merge fits the ring");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, tw = wave / RW;
@@ -495,51 +495,44 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
     l_run = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
   if (m_run == -INFINITY && l_run != 0.f) m_run = 0.f;  // only NaN scores
-  // the second token group's part goes to the first through the ring, which the
-  // copies past the last step (they read nothing) have left
-  float* const s_o = reinterpret_cast<float*>(smem);
-  float* const s_ml = s_o + RW * 32 * D;
+  // Each token group hands half of its columns to the other, which merges and stores them,
+  // through the ring, which the copies past the last step (they read nothing) have left.
+  constexpr int HT = D / 64;  // tiles of 32 columns in a half
+  f32x4_v* const s_o = reinterpret_cast<f32x4_v*>(smem);
+  float2* const s_ml = reinterpret_cast<float2*>(s_o + 4 * HT * 4 * 64);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __syncthreads();
-  if (tw == 1) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4) =
-            f32x4_v{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
-    if (hi == 0) {
-      s_ml[(rw * 32 + q) * 2] = m_run;
-      s_ml[(rw * 32 + q) * 2 + 1] = l_run;
-    }
-  }
-  __syncthreads();
-  if (tw == 1) return;
-  const float m1 = s_ml[(rw * 32 + q) * 2], l1 = s_ml[(rw * 32 + q) * 2 + 1];
-  const float m = fmaxf(m_run, m1);
-  const float c0 = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m);
-  const float c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - m);
-  m_run = m;
-  l_run = l_run * c0 + l1 * c1;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
+  for (int i = 0; i < HT; ++i)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const f32x4_v p = *reinterpret_cast<const f32x4_v*>(s_o + (((rw * (D / 32) + i) * 4 + g) * 64 + lane) * 4);
+      f32x4_v x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][4 * g + e] = o[i][4 * g + e] * c0 + p[e] * c1;
+      for (int e = 0; e < 4; ++e) x[e] = tw ? o[i][4 * g + e] : o[HT + i][4 * g + e];
+      s_o[((wave * HT + i) * 4 + g) * 64 + lane] = x;
     }
+  if (hi == 0) s_ml[wave * 32 + q] = make_float2(m_run, l_run);
+  __syncthreads();
   if (!real) return;
+  const int peer = rw + RW * (1 - tw);
+  const float2 ml = s_ml[peer * 32 + q];
+  const float m = fmaxf(m_run, ml.x);
+  const float c0 = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m);
+  const float c1 = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
   const int64_t to = ((int64_t)rb * a.n_heads + rh) * a.splits + split;
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
+  for (int i = 0; i < HT; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<f32x4_v*>(a.part_o + to * D + dt * 32 + g * 8 + hi * 4) =
-          f32x4_v{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
-  if (hi == 0) {
-    a.part_ml[to * 2] = m_run;
-    a.part_ml[to * 2 + 1] = l_run;
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_v y = s_o[((peer * HT + i) * 4 + g) * 64 + lane];
+      f32x4_v x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (tw ? o[HT + i][4 * g + e] : o[i][4 * g + e]) * c0 + y[e] * c1;
+      *reinterpret_cast<f32x4_v*>(a.part_o + to * D + (tw * HT + i) * 32 + g * 8 + hi * 4) = x;
+    }
+  if (hi == 0 && tw == 0) {
+    a.part_ml[to * 2] = m;
+    a.part_ml[to * 2 + 1] = l_run * c0 + ml.y * c1;
   }
 }
 
