@@ -628,22 +628,24 @@ __device__ __forceinline__ void merge_out_wave(const CacheAttnArgs& a, int h, in
   constexpr int LPR = D / 4, RPP = 64 / LPR, U = 32 / RPP;
   const int lane = threadIdx.x & 63;
   const int64_t row = ((int64_t)b * a.n_heads + h) * a.splits;
+  const __amdgpu_buffer_rsrc_t rows =  // past the last split: zeros, without traffic
+      __builtin_amdgcn_make_buffer_rsrc(a.part_o + row * D, 0, a.splits * D * 4, kRsrcWord3);
   f32x4_v v[U], o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (u * RPP < a.splits)  // uniform
-      v[u] = *reinterpret_cast<const f32x4_v*>(a.part_o + (row + min(u * RPP + lane / LPR, a.splits - 1)) * D + (lane % LPR) * 4);
+    v[u] = __builtin_bit_cast(f32x4_v, __builtin_amdgcn_raw_buffer_load_b128(rows, (u * 64 + lane) * 16, 0, 0));
   const float2 first = first_ml(a, a.part_ml + row * 2);
   const int n = splits_of(a, ctx_of(a, b));
-  float M, L;
-  merge_ml(nullptr, first, n, M, L);
-  const float w = lane < n && first.x != -INFINITY ? fast_exp2(first.x - M) : 0.f;
+  float M = lane < n ? first.x : -INFINITY;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (u * RPP < n) {
-      const float x = __shfl(w, u * RPP + lane / LPR, 64);
-      if (x != 0.f) o += v[u] * x;  // (a split without weight may hold anything)
-    }
+  for (int e = 32; e > 0; e >>= 1) M = fmaxf(M, __shfl_xor(M, e, 64));
+  const float w = lane < n && first.x != -INFINITY ? fast_exp2(first.x - M) : 0.f;
+  const float L = wave_sum(lane < n && first.x != -INFINITY ? first.y * w : 0.f);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const float x = __shfl(w, u * RPP + lane / LPR, 64);
+    if (x != 0.f) o += v[u] * x;  // (a split without weight may hold anything)
+  }
 #pragma unroll
   for (int e = LPR; e < 64; e <<= 1)
 #pragma unroll
@@ -700,7 +702,7 @@ __host__ __device__ __forceinline__ int merge_groups(int n_heads, int splits) {
   return splits <= kWaveSplits ? (n_heads + 3) / 4 : n_heads;
 }
 template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5))) void cache_attn_merge_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(256) void cache_attn_merge_kernel(CacheAttnArgs a) {
   const int i = blockIdx.x, groups = merge_groups(a.n_heads, a.splits);
   if (i >= groups) return add_weights(a, (i - groups) % a.n_kv_heads, blockIdx.y, (i - groups) / a.n_kv_heads);
   if (a.splits > kWaveSplits) return merge_out<D>(a, i, blockIdx.y);
