@@ -16,10 +16,9 @@
 // are one split, whose workgroup writes output and weights without a second kernel.
 //
 // Bound by HBM: every cached key and value is read once. MI355X, merge included: 8B heads, 32
-// sequences of 64 to 512 tokens behind 8192 22.3 us (72 MB: 3.2 TB/s; the prefix takes 19.5 us, of
-// which 3.7 are the first copies' way and 8 its eight steps, its partial results' merge 4); 13B
-// heads, 24 of up to 300 behind 2011 28.0 us (4.2 TB/s); with weights, 24 of 512 to 4096 behind 1000
-// 54.4 us (4.5 TB/s).
+// sequences of 64 to 512 tokens behind 8192 21.2 us (72 MB: 3.4 TB/s; in a kernel trace 19.4 and 3.9 for the
+// merge; the prefix's first copies take 3.7, its eight steps 8); 13B heads, 24 of up to 300 behind 2011
+// 27.5 us (4.3 TB/s); with weights, 24 of 512 to 4096 behind 1000 53.4 us (4.6 TB/s).
 #include "hs_device.h"
 #include "hs_kernels.h"
 
@@ -716,14 +715,16 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
   const int64_t rows = B * (n_heads / n_kv_heads), blocks = (prefix_len + 15) / 16;
   const int64_t slots = blocks * 16 + (max_ctx + 15) / 16 * 16;
   // Alone: a step of 256 slots at least as fast as splits and their merge at any batch; longer
-  // ones where a workgroup per CU has enough of them (64 and more for 3 and 4 steps) and not
-  // too many. MI355X, in a graph, splits and merge -> alone: 3 sequences of 97 tokens, 4 heads
-  // 7.5 -> 3.4 us; 32 of 200, 8 kv heads 14.0 -> 6.1; 24 of 200, 40 heads 16.4 -> 14.3; 32 of 1000, 8 kv
-  // heads 25.4 -> 19.6. Left to the splits: 4 of 1000, 8 kv heads 9.2 (12.6 alone); 24 of 300 + 100,
-  // 40 heads 18.2 (28.3).
+  // ones where the workgroups fill the chip (128 and more for 3 and 4 steps), at two to a
+  // CU in turn, or at one if each would read a prefix that the others have read. MI355X, in a graph, splits
+  // and merge -> alone: 3 sequences of 97 tokens, 4 heads 7.2 -> 3.4 us; 32 of 200, 8 kv heads 10.7 -> 6.1;
+  // 24 of 200, 40 heads 15.7 -> 14.4; 32 of 1000, 8 kv heads 23.9 -> 19.4; 28 of 400 behind 600 17.2 -> 13.5; 56 of
+  // 1000 38.4 -> 34.4. Left to the splits: 8 of 1000 10.6 (13.0 alone); 36 of 100 behind 900 13.2 (21.8), 48 of 400
+  // behind 600 19.2 (24.4).
   const int64_t groups = B * n_kv_heads;
-  p.direct = slots <= 256 || (groups <= 512 && slots <= (groups < 64 ? 512 : kDirect));
-  p.shared = !p.direct && B > 1 && prefix_len > 0;
+  const bool prefixed = B > 1 && prefix_len > 0;
+  p.direct = slots <= 256 || (groups <= (prefixed ? 256 : 512) && slots <= (groups < 128 ? 512 : kDirect));
+  p.shared = !p.direct && prefixed;
   p.lead_blocks = p.shared ? 0 : (int)blocks;
   p.own_blocks = p.direct ? kDirect / 16 : 8;
   p.prefix_tokens = 0;

@@ -281,9 +281,11 @@ SHARED = [
     ([17, 128, 129, 0, 1], 16, 32, 8, 128), ([100, 5], 640, 32, 32, 128), ([300, 0, 16, 127], 129, 8, 4, 128),
     ([33] * 9, 200, 16, 1, 128), ([2, 31], 500, 12, 1, 128), ([40, 7, 64], 333, 6, 2, 64), ([600, 1, 300], 1111, 6, 2, 64), ([200] * 19, 1040, 14, 2, 128),
     ([1025], 0, 32, 8, 128), ([1024], 0, 4, 4, 64), ([513, 300], 0, 8, 2, 128),
-    ([9000], 0, 4, 4, 64), ([5, 700], 9000, 2, 1, 128), ([8300, 1, 8190], 7, 4, 2, 128),  # more than 64 splits ([3] * 40, 300, 8, 2, 64),
+    ([9000], 0, 4, 4, 64), ([5, 700], 9000, 2, 1, 128), ([8300, 1, 8190], 7, 4, 2, 128),  # more than 64 splits
+    ([3] * 40, 300, 8, 2, 64),
     ([0] * 5, 1000, 10, 2, 128), ([700, 1300, 60], 15, 8, 8, 128), ([1, 2, 3] * 11, 513, 20, 4, 128), ([1] * 130, 90, 4, 1, 64),
-    ([5] * 33, 2100, 16, 4, 64), ([64] * 70, 700, 8, 2, 128), ([9, 0, 30], 4100, 4, 4, 128)]
+    ([5] * 33, 2100, 16, 4, 64), ([64] * 70, 700, 8, 2, 128), ([9, 0, 30], 4100, 4, 4, 128),
+    ([1024, 700, 3, 0] * 4, 0, 16, 8, 128), ([769, 1, 513, 0] * 5, 130, 8, 8, 64), ([40, 0, 33] * 11, 300, 8, 8, 64)]
 
 
 @pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED)
@@ -373,7 +375,8 @@ def test_attn_decode_shared_large_scores():
             assert np.all(np.abs(got[b] - o) <= tol), (prefix, b)
 
 
-@pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED[:3] + SHARED[4:14] + [([2000, 1025, 1024], 0, 8, 2, 128), ([1500, 3], 100, 4, 4, 64), ([9000, 20, 0], 30, 4, 2, 64)])
+@pytest.mark.parametrize("lens,prefix,nh,nkv,d", SHARED[:3] + SHARED[4:14] + SHARED[-3:] + [
+    ([2000, 1025, 1024], 0, 8, 2, 128), ([1500, 3], 100, 4, 4, 64), ([9000, 20, 0], 30, 4, 2, 64)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_attn_decode_weights(lens, prefix, nh, nkv, d, in_place):
     """Outputs as above; weights within the error of G probabilities and of the accumulation;
