@@ -24,6 +24,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kCopies = 8;        // of the first pass's histogram, by lane: most weights share a few exponents
 constexpr int kMovesHere = 1024;  // per row at most, in the selecting workgroup
 constexpr int kMovesPerGroup = 32;
+constexpr int kHeld = 32;  // keys of a lane held in LDS, of longer rows
 
 // Larger keys stay. A NaN is below every weight, a protected token above all.
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int64_t recent_from) {
@@ -89,16 +90,19 @@ __device__ __forceinline__ void move_tokens(const KvEvictArgs& a, F pair, int j0
 
 // K > 0: max_ctx is at most K * 1024, and a token's weight, position and key stay in
 // registers (wave w has tokens [64 w per, 64 (w + 1) per), per = ceil(max_ctx / 1024) to a
-// lane; they are requested together with the row's length). K = 0: longer rows, read
-// again in every pass.
+// lane; they are requested together with the row's length). K = 0: longer rows, whose
+// keys stay in LDS, 32768 of them; the others are formed again in every pass, the next eight to
+// a lane requested before these are used. MI355X, all read again in every pass -> so: 8 rows of
+// 17536 tokens down to 4000 55.6 -> 33.2 us, of 60000 down to 8000 162 -> 90.
 template <int D, int K, bool MOVE>
 __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a) {
   constexpr int R = K > 0 ? K : 1;
-  constexpr int kMoves = MOVE ? kMovesHere : 4096;  // listed in LDS
+  constexpr int kMoves = MOVE || K == 0 ? kMovesHere : 4096;  // listed in LDS
   __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * (kCopies + 3)];
   __shared__ __attribute__((aligned(16))) uint32_t s_wave[3][kWaves];
   __shared__ uint32_t s_pick[4][3];
   __shared__ int s_table[R * 64], s_hole[kMoves], s_mover[kMoves];
+  __shared__ uint32_t s_key[K > 0 ? 1 : kHeld * kThreads];
   const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = (int64_t)b * a.n_kv_heads + kh;
@@ -125,34 +129,68 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   if (kh == 0 && tid == 0) a.ctx_out[b] = kept;
   if constexpr (K == 0) per = (n + kThreads - 1) / kThreads;
   const int first = wave * 64 * per + lane;
-  // f(token, weight, position, key) for every token of the lane
   uint32_t keys[R];
   if constexpr (K > 0) {
 #pragma unroll
     for (int i = 0; i < K; ++i) keys[i] = evict_key(ws[i], ps[i], a.sinks, recent_from);
   }
+  // f(token, key) for every token of the lane; for K = 0 from memory from the lane's i0-th on
+  const auto each_from = [&](int i0, auto f) {
+    constexpr int U = 8;
+    float w[U];
+    int p[U];
+    const auto load = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = min(first + (i + u) * 64, n - 1);
+        w[u] = acc[t];
+        p[u] = pos[t];
+      }
+    };
+    if (i0 < per) load(i0);
+    for (int i = i0; i < per; i += U) {
+      uint32_t k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) k[u] = evict_key(w[u], p[u], a.sinks, recent_from);
+      load(i + U);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u < per) f(i + u, k[u]);
+    }
+  };
   const auto each = [&](auto f) {
     if constexpr (K > 0) {
 #pragma unroll
       for (int i = 0; i < K; ++i)
-        if (i < per) f(first + i * 64, ws[i], ps[i], keys[i]);
+        if (i < per) f(first + i * 64, keys[i]);
     } else {
-      for (int i = 0; i < per; ++i) {
-        const int t = first + i * 64, u = min(t, n - 1);
-        const float w = acc[u];
-        const int p = pos[u];
-        f(t, w, p, evict_key(w, p, a.sinks, recent_from));
+#pragma unroll 4
+      for (int i = 0; i < min(per, kHeld); ++i) f(first + i * 64, s_key[i * kThreads + tid]);
+      each_from(kHeld, [&](int i, uint32_t k) { f(first + i * 64, k); });
+    }
+  };
+  // the weights and positions below `end`, as they are
+  const auto copy = [&](int end) {
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int t = first + i * 64;
+        if (i >= per || t >= end) continue;
+        if (acc_out != acc) acc_out[t] = ws[i];
+        if (pos_out != pos) pos_out[t] = ps[i];
       }
+    } else {
+#pragma unroll 4
+      for (int t = tid; t < end; t += kThreads)
+        if (acc_out != acc) acc_out[t] = acc[t];
+#pragma unroll 4
+      for (int t = tid; t < end; t += kThreads)
+        if (pos_out != pos) pos_out[t] = pos[t];
     }
   };
   if (n <= a.keep) {
     if (!MOVE && tid == 0) a.counts[row] = 0;
-    each([&](int t, float w, int p, uint32_t) {
-      if (t >= n) return;
-      if (acc_out != acc) acc_out[t] = w;
-      if (pos_out != pos) pos_out[t] = p;
-    });
-    return;
+    return copy(n);
   }
 
   // the keep-th largest key, and how many of the tokens with that key stay
@@ -162,9 +200,17 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     constexpr int copies = decltype(copies_)::value;
     const int shift = 24 - 8 * pass;
     uint32_t* const hist = s_hist + (pass ? 256 * (kCopies + pass - 1) : 0);
-    each([&](int t, float, int, uint32_t k) {
+    const auto count = [&](int t, uint32_t k) {
       if (t < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & 255) * copies + (lane & (copies - 1))], 1u);
-    });
+    };
+    if constexpr (K == 0 && copies > 1) {  // the first pass
+      each_from(0, [&](int i, uint32_t k) {
+        if (i < kHeld) s_key[i * kThreads + tid] = k;
+        count(first + i * 64, k);
+      });
+    } else {
+      each(count);
+    }
     __syncthreads();
     if (wave == 0) {  // lane l has bins 255 - 4 l down to 252 - 4 l
       uint32_t c[4], sum = 0;
@@ -211,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   uint32_t all, eq = 0;
   const bool ties = s_pick[3][2] != need;  // uniform
   if (ties) {
-    each([&](int t, float, int, uint32_t k) { eq += __popcll(__ballot(t < n && k == prefix)); });
+    each([&](int t, uint32_t k) { eq += __popcll(__ballot(t < n && k == prefix)); });
     if (lane == 0) s_wave[0][wave] = eq;
     __syncthreads();
     eq = waves_before(s_wave[0], wave, &all);
@@ -226,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     return s;
   };
   uint32_t holes = 0, movers = 0;
-  each([&](int t, float, int, uint32_t k) {
+  each([&](int t, uint32_t k) {
     const bool s = stays(k, t);
     holes += __popcll(__ballot(t < a.keep && !s));
     movers += __popcll(__ballot(t >= a.keep && s));
@@ -242,8 +288,9 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   int2* const pairs = reinterpret_cast<int2*>(a.lists) + row * a.cap;
   const bool in_lds = a.cap <= kMoves;
   eq = eq0;
-  // the holes, the tokens that fill them, and the weights of what keeps its slot
-  each([&](int t, float w, int p, uint32_t k) {
+  copy(a.keep);  // (a hole's are written again below)
+  // the holes and the tokens that fill them
+  each([&](int t, uint32_t k) {
     const bool s = stays(k, t);
     const int t_first = __builtin_amdgcn_readfirstlane(t);
     if (t_first < a.keep) {
@@ -255,10 +302,6 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
         else pairs[j].y = t;
       }
       holes += __popcll(m);
-      if (t < a.keep && s) {
-        if (acc_out != acc) acc_out[t] = w;
-        if (pos_out != pos) pos_out[t] = p;
-      }
     }
     if (t_first + 63 >= a.keep) {
       const bool mover = t >= a.keep && s;

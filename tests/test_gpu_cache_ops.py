@@ -439,7 +439,8 @@ def evicted(acc, pos, n, seen, keep, sinks, recent):
 
 EVICT = [([5], 8, 0, 0, 4, 64), ([9, 8, 7, 0, 1], 8, 1, 2, 4, 64), ([33, 40, 2], 1, 0, 0, 2, 128), ([50], 49, 4, 40, 8, 128),
          ([1023, 1024, 1025, 1026], 1024, 4, 100, 1, 64), ([3000, 2049, 100], 2048, 4, 256, 2, 128), ([5000], 700, 0, 0, 2, 128),
-         ([12000, 11000], 2048, 4, 64, 2, 64), ([300, 260], 100, 70, 70, 3, 64), ([40000], 16, 2, 2, 1, 64), ([20000, 900, 17001], 800, 4, 50, 1, 128), ([17000], 9000, 0, 0, 1, 64), ([17] * 30, 16, 0, 16, 3, 128)]
+         ([12000, 11000], 2048, 4, 64, 2, 64), ([300, 260], 100, 70, 70, 3, 64), ([40000], 16, 2, 2, 1, 64), ([20000, 900, 17001], 800, 4, 50, 1, 128), ([17000], 9000, 0, 0, 1, 64), ([17] * 30, 16, 0, 16, 3, 128),
+         ([40000, 0, 32769, 5001, 5000], 5000, 4, 300, 2, 64)]
 
 
 def evict_case(lens, keep, sinks, recent, nkv, d, seed, kind):
