@@ -134,7 +134,8 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
 #pragma unroll
     for (int i = 0; i < K; ++i) keys[i] = evict_key(ws[i], ps[i], a.sinks, recent_from);
   }
-  // f(token, key) for every token of the lane; for K = 0 from memory from the lane's i0-th on
+  // f(token, key, index in the registers) for every token of the lane; for K = 0 from memory
+  // from the lane's i0-th on
   const auto each_from = [&](int i0, auto f) {
     constexpr int U = 8;
     float w[U];
@@ -162,35 +163,31 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     if constexpr (K > 0) {
 #pragma unroll
       for (int i = 0; i < K; ++i)
-        if (i < per) f(first + i * 64, keys[i]);
+        if (i < per) f(first + i * 64, keys[i], i);
     } else {
 #pragma unroll 4
-      for (int i = 0; i < min(per, kHeld); ++i) f(first + i * 64, s_key[i * kThreads + tid]);
-      each_from(kHeld, [&](int i, uint32_t k) { f(first + i * 64, k); });
+      for (int i = 0; i < min(per, kHeld); ++i) f(first + i * 64, s_key[i * kThreads + tid], 0);
+      each_from(kHeld, [&](int i, uint32_t k) { f(first + i * 64, k, 0); });
     }
   };
-  // the weights and positions below `end`, as they are
-  const auto copy = [&](int end) {
-    if constexpr (K > 0) {
-#pragma unroll
-      for (int i = 0; i < K; ++i) {
-        const int t = first + i * 64;
-        if (i >= per || t >= end) continue;
-        if (acc_out != acc) acc_out[t] = ws[i];
-        if (pos_out != pos) pos_out[t] = ps[i];
-      }
-    } else {
+  const auto put = [&](int t, float w, int p) {
+    if (acc_out != acc) acc_out[t] = w;
+    if (pos_out != pos) pos_out[t] = p;
+  };
+  const auto copy = [&](int end) {  // K = 0
 #pragma unroll 4
-      for (int t = tid; t < end; t += kThreads)
-        if (acc_out != acc) acc_out[t] = acc[t];
+    for (int t = tid; t < end; t += kThreads)
+      if (acc_out != acc) acc_out[t] = acc[t];
 #pragma unroll 4
-      for (int t = tid; t < end; t += kThreads)
-        if (pos_out != pos) pos_out[t] = pos[t];
-    }
+    for (int t = tid; t < end; t += kThreads)
+      if (pos_out != pos) pos_out[t] = pos[t];
   };
   if (n <= a.keep) {
     if (!MOVE && tid == 0) a.counts[row] = 0;
-    return copy(n);
+    if constexpr (K == 0) return copy(n);
+    return each([&](int t, uint32_t, int i) {
+      if (t < n) put(t, ws[i], ps[i]);
+    });
   }
 
   // the keep-th largest key, and how many of the tokens with that key stay
@@ -200,13 +197,13 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     constexpr int copies = decltype(copies_)::value;
     const int shift = 24 - 8 * pass;
     uint32_t* const hist = s_hist + (pass ? 256 * (kCopies + pass - 1) : 0);
-    const auto count = [&](int t, uint32_t k) {
+    const auto count = [&](int t, uint32_t k, int) {
       if (t < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & 255) * copies + (lane & (copies - 1))], 1u);
     };
     if constexpr (K == 0 && copies > 1) {  // the first pass
       each_from(0, [&](int i, uint32_t k) {
         if (i < kHeld) s_key[i * kThreads + tid] = k;
-        count(first + i * 64, k);
+        count(first + i * 64, k, i);
       });
     } else {
       each(count);
@@ -257,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   uint32_t all, eq = 0;
   const bool ties = s_pick[3][2] != need;  // uniform
   if (ties) {
-    each([&](int t, uint32_t k) { eq += __popcll(__ballot(t < n && k == prefix)); });
+    each([&](int t, uint32_t k, int) { eq += __popcll(__ballot(t < n && k == prefix)); });
     if (lane == 0) s_wave[0][wave] = eq;
     __syncthreads();
     eq = waves_before(s_wave[0], wave, &all);
@@ -272,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
     return s;
   };
   uint32_t holes = 0, movers = 0;
-  each([&](int t, uint32_t k) {
+  each([&](int t, uint32_t k, int) {
     const bool s = stays(k, t);
     holes += __popcll(__ballot(t < a.keep && !s));
     movers += __popcll(__ballot(t >= a.keep && s));
@@ -288,9 +285,9 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
   int2* const pairs = reinterpret_cast<int2*>(a.lists) + row * a.cap;
   const bool in_lds = a.cap <= kMoves;
   eq = eq0;
-  copy(a.keep);  // (a hole's are written again below)
-  // the holes and the tokens that fill them
-  each([&](int t, uint32_t k) {
+  if constexpr (K == 0) copy(a.keep);  // (a hole's are written again below)
+  // the holes, the tokens that fill them, and the weights of what keeps its slot
+  each([&](int t, uint32_t k, int i) {
     const bool s = stays(k, t);
     const int t_first = __builtin_amdgcn_readfirstlane(t);
     if (t_first < a.keep) {
@@ -302,6 +299,7 @@ __global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a
         else pairs[j].y = t;
       }
       holes += __popcll(m);
+      if (K > 0 && t < a.keep && s) put(t, ws[i], ps[i]);
     }
     if (t_first + 63 >= a.keep) {
       const bool mover = t >= a.keep && s;
