@@ -21,7 +21,6 @@ namespace hs {
 
 namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kCopies = 8;        // of the first pass's histogram, by lane: most weights share a few exponents
 constexpr int kMovesHere = 1024;  // per row at most, in the selecting workgroup
 constexpr int kMovesPerGroup = 32;
 constexpr int kHeld = 32;  // keys of a lane held in LDS, of longer rows
@@ -90,13 +89,18 @@ __device__ __forceinline__ void move_tokens(const KvEvictArgs& a, F pair, int j0
 
 // K > 0: max_ctx is at most K * 1024, and a token's weight, position and key stay in
 // registers (wave w has tokens [64 w per, 64 (w + 1) per), per = ceil(max_ctx / 1024) to a
-// lane; they are requested together with the row's length). K = 0: longer rows, whose
-// keys stay in LDS, 32768 of them; the others are formed again in every pass, the next eight to
-// a lane requested before these are used. MI355X, all read again in every pass -> so: 8 rows of
-// 17536 tokens down to 4000 55.6 -> 33.2 us, of 60000 down to 8000 162 -> 90.
+// lane; they are requested together with the row's length); up to K = 8 in 64 registers, so
+// that a CU holds two workgroups (MI355X, K = 16 -> 8: 960 rows of 4097 to 4224 tokens down to 4096 63.9 -> 39.6
+// us, 8 of 4500 to 5000 14.4 -> 12.0; K = 4 -> 2: 256 rows of 1025 to 1100 down to 1024 9.2 -> 8.6). K = 0: longer
+// rows, whose keys stay in LDS, 32768 of them; the others are formed again in every pass, the next
+// eight to a lane requested before these are used (all read again in every pass -> so: 8
+// rows of 17536 tokens down to 4000 55.6 -> 33.2 us, of 60000 down to 8000 162 -> 90).
 template <int D, int K, bool MOVE>
-__global__ __launch_bounds__(kThreads) void kv_evict_select_kernel(KvEvictArgs a) {
+__global__ __launch_bounds__(kThreads, K == 0 || K == 16 ? 4 : 8) void kv_evict_select_kernel(KvEvictArgs a) {
   constexpr int R = K > 0 ? K : 1;
+  // of the first pass's histogram, by lane: most weights share a few exponents (four take fewer
+  // registers and reads, eight fewer turns at one address, 38.2 us for 38.8 at K = 16)
+  constexpr int kCopies = K == 16 ? 8 : 4;
   constexpr int kMoves = MOVE || K == 0 ? kMovesHere : 4096;  // listed in LDS
   __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * (kCopies + 3)];
   __shared__ __attribute__((aligned(16))) uint32_t s_wave[3][kWaves];
@@ -357,7 +361,9 @@ hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
       if (here) hipLaunchKernelGGL((kv_evict_select_kernel<D, K, true>), grid, dim3(kThreads), 0, s, a);
       else hipLaunchKernelGGL((kv_evict_select_kernel<128, K, false>), grid, dim3(kThreads), 0, s, a);  // (no use of D)
     };
-    if (a.max_ctx <= 4 * kThreads) select(std::integral_constant<int, 4>{});
+    if (a.max_ctx <= 2 * kThreads) select(std::integral_constant<int, 2>{});
+    else if (a.max_ctx <= 4 * kThreads) select(std::integral_constant<int, 4>{});
+    else if (a.max_ctx <= 8 * kThreads) select(std::integral_constant<int, 8>{});
     else if (a.max_ctx <= 16 * kThreads) select(std::integral_constant<int, 16>{});
     else select(std::integral_constant<int, 0>{});
     if (!here)
