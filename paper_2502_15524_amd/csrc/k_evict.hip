@@ -349,10 +349,9 @@ hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
     return hipErrorInvalidValue;
   const dim3 grid(a.n_kv_heads, a.B);
   // One launch for up to 512 moves a row, to 1024 where the rows fill the chip. MI355X, moved in the
-  // second kernel -> in the first: 32 sequences of 600 to 900 down to 500, 8 kv heads 18.2 -> 16.3 us; 64 of
-  // 1000 to 1500 down to 800 36.6 -> 33.6; 8 of 600 to 900 9.8 -> 10.2, but a launch (4 us of the host's
-  // time) less; 16 of 2000 to 6000 down to 1500 36.6 -> 51.9 and 1 of 1500 down to 1000, 32 kv heads 10.7 ->
-  // 13.3, which the rule leaves to the second or pays for the launch.
+  // second kernel -> in the first: 32 sequences of 600 to 900 down to 500, 8 kv heads 18.0 -> 15.8 us; 64 of
+  // 1000 to 1500 down to 800 35.5 -> 32.8; 8 of 600 to 900 9.3 -> 9.7 and 1 of 1500 down to 1000, 32 kv heads
+  // 10.1 -> 12.5, but a launch (4 us of the host's time) less.
   const bool here = a.cap <= 512 || (a.cap <= kMovesHere && (int64_t)a.B * a.n_kv_heads >= 256);
   const auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;
