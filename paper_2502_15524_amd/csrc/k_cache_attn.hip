@@ -55,16 +55,15 @@ __device__ __forceinline__ v4i_t scalar_rsrc(const void* p, uint32_t bytes) {
 }
 
 // Two probabilities as sums of two bf16 each: the upper 8 bits of the significand, and the
-// rest rounded, at most 2^-15 of the probability off. The second is never zero, so that a value
-// of infinity gives infinity (times zero: NaN); a probability of 2^-126 more changes nothing.
+// rest rounded, at most 2^-15 of the probability off. The last bit is set, so that the rest is zero
+// for zero alone (below 2^-103 it may underflow): an infinite value gives infinity, where zero times it were NaN.
 // One rounding to bf16 instead left outputs 0.0020 to 0.0022 of the norm off, 0.0017 now, what their
 // own rounding takes; MI355X: 8B heads, 32 sequences behind 8192 tokens 21.7 -> 22.7 us (a prefix
 // of many query heads is near the matrix instructions' rate), 13B heads and single sequences unchanged.
 __device__ __forceinline__ void split2bf(float x, float y, uint32_t& big, uint32_t& rest) {
-  constexpr float kLeast = 1.17549435e-38f;
   const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
   big = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-  rest = pack2bf(fmaxf(x - hi_bf(a), kLeast), fmaxf(y - hi_bf(b), kLeast));
+  rest = pack2bf(__uint_as_float(a | 1) - hi_bf(a), __uint_as_float(b | 1) - hi_bf(b));
 }
 
 // 16 bytes read once per call (a non-temporal load)

@@ -69,3 +69,21 @@ def test_an_infinite_value_gives_infinity(lens, prefix, d):
     if prefix:
         want[:, 0, :, 21] = -np.inf
     assert np.array_equal(np.where(np.isfinite(got), 0, got), want)
+
+
+@pytest.mark.parametrize("lens,prefix", [([40, 3], 0), ([40, 3], 300), ([900] * 3, 0), ([900, 700], 1500)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_large_value_without_probability_adds_nothing(lens, prefix, d):
+    """A token whose score is several hundred below the others has probability zero in float32, and
+    in float64 less than 10^-100: its values of 2^127 add nothing to any output."""
+    c = sharp(lens, prefix, 4, 4, d, 6)
+    c.k[0][prefix + 17] = -64 * np.where(c.q[0] < 0, -1, 1).reshape(4, d)
+    c.v[0][prefix + 17] = 2.0 ** 127
+    c._put(c.table[0, 1], 1, c.k[0][prefix + 17], c.v[0][prefix + 17])
+    got = run_shared(c)
+    q = c.q[0].reshape(4, 1, d).astype(np.float64)
+    s = (q @ c.k[0].astype(np.float64).transpose(1, 2, 0)) / np.sqrt(d)
+    assert np.all(s[:, :, prefix + 17] < s.max(axis=2) - 200)
+    o, tol, _, _ = c.exact(0, [prefix + 17])
+    assert np.all(np.abs(tol) < 1)
+    assert np.all(np.abs(got[0] - o) <= tol), np.abs(got[0] - o).max()
