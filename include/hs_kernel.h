@@ -185,8 +185,9 @@ typedef struct {
 /* cos_t[p][i] = magnitude cos(p w_i'), sin_t[p][i] = magnitude sin(p w_i') for p <
  * max_pos, i < rot_dim / 2: device float32 [max_pos][rot_dim / 2], 16-byte
  * aligned. rot_dim: 8 to 128, a multiple of 8; base > 1; scaling: host, NULL = plain
- * with magnitude 1. Angles are formed in float64, so far positions are as exact as
- * near ones. */
+ * with magnitude 1. The angle per position is formed in float64 and held as a 64-bit
+ * fraction of a turn, and entries are within 6 x 2^-24 of their value for it: far
+ * positions are as exact as near ones, and small sines as large ones. */
 hs_status hs_k_rope_tables(float* cos_t, float* sin_t, int32_t max_pos, int32_t rot_dim,
                            double base, const hs_rope_scaling* scaling, void* stream);
 

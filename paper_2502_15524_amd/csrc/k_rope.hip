@@ -9,28 +9,35 @@ namespace hs {
 //
 // Entry (p, i): cos and sin of p w_i, times a magnitude. The angle is formed in
 // turns as a 64-bit fraction, p times w_i / 2 pi modulo 1 (at position 131072 a float32
-// angle would be off by 0.008 rad; this one is by 2^-32 turns), and whole quarter
-// turns are taken off before the rounding to float32, which leaves at most pi / 4 for the
-// two Taylor polynomials (their first dropped terms are below 2e-9 and 2e-10). Bound by
-// the stores, 8 bytes per entry: 131072 positions of 64 pairs 11.9 us, 5.7 TB/s, on MI355X
-// (12.3 with the angles in float64; a fill of the same bytes takes 9.8).
+// angle would be off by 0.008 rad), and whole quarter turns are taken off before the
+// rounding to float32, which is of all 64 bits, so that a small sine has as many good bits as a
+// large one. That leaves at most half a quarter, y, for the two Taylor polynomials of pi / 2 y (their
+// first dropped terms are below 2e-9 and 2e-10). Bound by
+// the stores, 8 bytes per entry: 131072 positions of 64 pairs 12.0 us, 5.6 TB/s, on MI355X
+// (12.3 with the angles in float64, 11.9 of 32 bits of the fraction, whose least sines were 0.4 %
+// off and more; a fill of the same bytes takes 9.8).
 
 struct RopeFreq {
   uint64_t turns[64];  // w_i / 2 pi in units of 2^-64
 };
 
 __device__ __forceinline__ void sincos_turns(uint64_t turns, float m, float& c, float& s) {
-  const uint32_t t = (uint32_t)(turns >> 32), q = (t + 0x20000000u) >> 30;
-  const float x = (float)(int32_t)(t << 2) * (1.57079632679f / 4294967296.f);  // |x| <= pi / 4
-  const float z = x * x;
-  float sp = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
-  sp = fmaf(z, sp, 8.33333333e-3f);
-  sp = fmaf(z, sp, -1.66666667e-1f);
-  sp = fmaf(x * z, sp, x);
-  float cp = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
-  cp = fmaf(z, cp, -1.38888889e-3f);
-  cp = fmaf(z, cp, 4.16666667e-2f);
-  cp = fmaf(z, cp, -0.5f);
+  constexpr double H = 1.57079632679489661923;
+  constexpr float h = (float)H, h_rest = (float)(H - (double)h);
+  const uint32_t up = (uint32_t)(turns >> 32), low = (uint32_t)turns << 2;
+  const uint32_t q = (up + 0x20000000u) >> 30;
+  // the part of a quarter left, 2^32 big + rest in units of 2^-64 (big saturates half a unit early)
+  const int big = __builtin_elementwise_add_sat((int)(turns >> 30), (int)(low >> 31)), rest = (int)low;
+  const float y = fmaf((float)big, 0x1p-32f, (float)rest * 0x1p-64f);  // |y| <= 1 / 2
+  const float z = y * y;
+  float sp = fmaf(z, (float)(H * H * H * H * H * H * H * H * H / 362880), (float)(-H * H * H * H * H * H * H / 5040));
+  sp = fmaf(z, sp, (float)(H * H * H * H * H / 120));
+  sp = fmaf(z, sp, (float)(-H * H * H / 6));
+  sp = fmaf(y, h, y * fmaf(z, sp, h_rest));
+  float cp = fmaf(z, (float)(-H * H * H * H * H * H * H * H * H * H / 3628800), (float)(H * H * H * H * H * H * H * H / 40320));
+  cp = fmaf(z, cp, (float)(-H * H * H * H * H * H / 720));
+  cp = fmaf(z, cp, (float)(H * H * H * H / 24));
+  cp = fmaf(z, cp, (float)(-H * H / 2));
   cp = fmaf(z, cp, 1.0f);
   const float a = q & 1 ? sp : cp, b = q & 1 ? cp : sp;
   // quarters 1 and 2 turn the cosine's sign, 2 and 3 the sine's

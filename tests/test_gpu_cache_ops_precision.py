@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from tests import gpu_util as G
-from tests.test_gpu_cache_ops import BF, F32, Cache, run_shared
+from tests.test_gpu_cache_ops import BF, F32, Cache, _hs, host, run_shared, turns
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +87,29 @@ def test_a_large_value_without_probability_adds_nothing(lens, prefix, d):
     o, tol, _, _ = c.exact(0, [prefix + 17])
     assert np.all(np.abs(tol) < 1)
     assert np.all(np.abs(got[0] - o) <= tol), np.abs(got[0] - o).max()
+
+
+@pytest.mark.parametrize("rot,base,kind,factor,original", [
+    (128, 500000.0, "linear", 8.0, 0), (128, 500000.0, "bands", 8.0, 8192), (64, 10000.0, "plain", 1.0, 0), (16, 1e9, "plain", 1.0, 0),
+    (128, 1e12, "linear", 1e4, 0), (96, 10000.0, "yarn", 16.0, 256), (8, 2.0, "ntk", 32.0, 0)])
+def test_small_angles_are_as_exact_as_large_ones(rot, base, kind, factor, original):
+    """|error| <= 6 x 2^-24 of the value: two half steps from the 64-bit fraction to float32, one of
+    the polynomial's sum, one of its inner terms together (a fifth of it at most), the
+    magnitude's and the product's. The fraction itself: 2^-64 of a turn and 2^-50 of the
+    frequency (float64) a position. At the first positions the slowest pairs turn by less than
+    2^-32, and their sines are that small."""
+    torch = G.torch()
+    hs = _hs()
+    sc = hs.rope_scaling(kind, factor=factor, original_ctx=original)
+    w = turns(rot, base, kind, factor, original, sc.low, sc.high)
+    n = 200
+    out = torch.zeros((2, n, rot // 2), dtype=torch.float32, device="cuda")
+    hs.hs_k_rope_tables(out[0].data_ptr(), out[1].data_ptr(), n, rot, base, sc, G.stream_ptr())
+    got = host(out).astype(np.float64)
+    pos = np.arange(n, dtype=np.longdouble)[:, None]
+    ang = pos * w
+    for at, f in ((0, np.cos), (1, np.sin)):
+        want = f(ang) * sc.magnitude
+        tol = 6 * F32 * np.abs(want) + sc.magnitude * pos * (6.3 * 2.0 ** -64 + w * 2.0 ** -50)
+        off = np.abs(got[at] - want)
+        assert np.all(off <= tol), (at, np.unravel_index(np.argmax(off - tol), off.shape), (off / np.maximum(tol, 1e-30)).max())
