@@ -258,7 +258,7 @@ hs_status hs_k_attn_decode_weights(const void* q, int64_t ldq, const void* pool,
  * tokens are copied); they may be acc and pos themselves, with the same stride.
  * ctx_out[b] = min(ctx[b], keep), and may not be ctx. The sequences' own blocks are
  * distinct. stride >= max_ctx, out_stride >= min(keep, max_ctx); keep >= 1, sinks and
- * recent >= 0. A move from or to a block outside the pool is left out. */
+ * recent >= 0; at most 2^25 moves a row: min(keep, max_ctx - keep). A move from or to a block outside the pool is left out. */
 hs_status hs_k_kv_evict_ws(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx,
                            uint64_t* bytes);
 hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_t* block_table,

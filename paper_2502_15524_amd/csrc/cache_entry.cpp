@@ -250,16 +250,17 @@ extern "C" hs_status hs_k_attn_decode_weights(
 }
 
 namespace {
+// moves a row can have
+int64_t evict_cap(int32_t keep, int32_t max_ctx) {
+  return std::max<int64_t>(0, std::min<int64_t>(keep, (int64_t)max_ctx - keep));
+}
 hs_status evict_sizes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
   if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || keep < 1 || max_ctx < 1 || max_ctx > 1 << 30)
     return fail(HS_EINVAL, "bad arguments");
   if ((double)B * n_kv_heads * max_ctx > (double)(1ll << 48))
     return fail(HS_EINVAL, "too many sequences, heads and tokens");
+  if (evict_cap(keep, max_ctx) > kEvictMoves) return fail(HS_EINVAL, "more than 2^25 tokens of a row can move");
   return HS_OK;
-}
-// moves a row can have
-int64_t evict_cap(int32_t keep, int32_t max_ctx) {
-  return std::max<int64_t>(0, std::min<int64_t>(keep, (int64_t)max_ctx - keep));
 }
 uint64_t evict_bytes(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx) {
   return 4ull * B * n_kv_heads * (2 * evict_cap(keep, max_ctx) + 1);

@@ -204,6 +204,7 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
                               int64_t prefix_len, int64_t max_ctx, bool weights);
 hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStream_t s);
 
+constexpr int kEvictMoves = 1 << 25;  // of a row at most: a move's 16-byte chunks are counted in 32 bits
 struct KvEvictArgs {
   bf16_t* pool; int pool_blocks;
   const int32_t* block_table;              // [B][max_blocks]

@@ -68,6 +68,7 @@ __device__ __forceinline__ void move_tokens(const KvEvictArgs& a, F pair, int j0
   constexpr int CH = D / 4, U = 4;  // 16-byte chunks of a token
   const int c = threadIdx.x % CH;
   static_assert(THREADS % CH == 0, "a thread's chunks are alike");
+  static_assert((int64_t)kEvictMoves * CH + U * THREADS < 1ll << 31, "chunks are counted in 32 bits");
   for (int i0 = j0 * CH; i0 < j1 * CH; i0 += U * THREADS) {
     pack8 v[U];
     int2 p[U];
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(256) void kv_evict_move_kernel(KvEvictArgs a) {
 hipError_t kv_evict(const KvEvictArgs& a, hipStream_t s) {
   if (a.B <= 0) return hipSuccess;
   if ((a.D != 64 && a.D != 128) || a.n_kv_heads < 1 || a.n_kv_heads > 65535 || a.B > 65535 ||
-      a.keep < 1 || a.cap < 0 || a.cap >= 1 << 28)  // (2^32 threads of a launch)
+      a.keep < 1 || a.cap < 0 || a.cap > kEvictMoves)
     return hipErrorInvalidValue;
   const dim3 grid(a.n_kv_heads, a.B);
   // One launch for up to 512 moves a row, to 1024 where the rows fill the chip. MI355X, moved in the

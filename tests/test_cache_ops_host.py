@@ -110,3 +110,15 @@ def test_evict_workspace():
     refused(hs.HS_ERANGE, hs.hs_k_kv_evict, **(EVICT | dict(ws_bytes=need - 1)))
     refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 2, 8, 0, 64)
     refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 2, 8, 4, 0)
+
+
+def test_evictions_of_more_than_2_25_moves_are_refused():
+    """A row's moves are counted in 16-byte chunks, 32 of a token of 128 elements, in 32 bits: 2^26 of them
+    would overflow. Few moves of a long row, or of one that keeps nearly all, are as before."""
+    many = dict(max_blocks=1 << 26, stride=1 << 30, out_stride=1 << 30)
+    for keep, max_ctx in ((1 << 26, 1 << 27), (1 << 27, 1 << 28), ((1 << 25) + 1, (1 << 26) + 2), (1 << 29, 1 << 30)):
+        refused(hs.HS_EINVAL, hs.hs_k_kv_evict_ws, 1, 1, keep, max_ctx)
+        refused(hs.HS_EINVAL, hs.hs_k_kv_evict, **(EVICT | many | dict(B=1, n_kv_heads=1, keep=keep, max_ctx=max_ctx)))
+    for keep, max_ctx in ((1 << 25, 1 << 26), (1 << 25, 1 << 30), ((1 << 30) - (1 << 25), 1 << 30), (2048, 1 << 30)):
+        moves = min(keep, max_ctx - keep)
+        assert hs.hs_k_kv_evict_ws(1, 1, keep, max_ctx) == 4 * (2 * moves + 1)
