@@ -152,7 +152,9 @@ hs_status cache_attn_ws(int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t 
   if (!bytes) return fail(HS_EINVAL, "bad arguments");
   const hs_status r = cache_attn_sizes(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx);
   if (r != HS_OK) return r;
-  *bytes = 4ull * cache_attn_plan(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx, weights).floats;
+  const CacheAttnPlan p = cache_attn_plan(B, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx, weights);
+  if (!p.fits) return fail(HS_EINVAL, "too many sequences, heads and tokens for a launch");
+  *bytes = 4ull * p.floats;
   return HS_OK;
 }
 
@@ -180,6 +182,7 @@ hs_status cache_attn_call(CacheAttnArgs a, bool weights, void* ws, uint64_t ws_b
   }
   const CacheAttnPlan p =
       cache_attn_plan(a.B, a.n_heads, a.n_kv_heads, a.D, a.prefix_len, a.max_ctx, weights);
+  if (!p.fits) return fail(HS_EINVAL, "too many sequences, heads and tokens for a launch");
   const hs_status w = ws_ok(ws, ws_bytes, 4ull * p.floats);
   if (w != HS_OK) return w;
   return done(cache_attn(a, p, static_cast<float*>(ws), static_cast<hipStream_t>(stream)), "cache attention");

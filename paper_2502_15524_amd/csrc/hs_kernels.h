@@ -199,6 +199,8 @@ struct CacheAttnPlan {
   int own_blocks;                          // per split of a sequence
   int64_t prefix_splits, own_splits, splits, score_stride;
   int64_t part_o, part_ml, scores, floats;
+  int64_t groups, merge_groups;            // workgroups of the launches, merge_groups of each sequence
+  bool fits;                               // they are within what a launch takes
 };
 CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t D,
                               int64_t prefix_len, int64_t max_ctx, bool weights);

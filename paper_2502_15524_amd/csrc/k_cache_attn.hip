@@ -762,19 +762,18 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
   p.part_ml = parts * D;
   p.scores = (p.part_ml + parts * 2 + 3) / 4 * 4;
   p.floats = std::max<int64_t>(4, p.scores + B * n_heads * p.score_stride);
+  p.groups = (p.prefix_splits * ((rows + kTileRows - 1) / kTileRows) + B * p.own_splits) * n_kv_heads;
+  const int64_t chunks = weights ? (max_ctx + 1023) / 1024 : 0;
+  p.merge_groups = merge_groups((int)n_heads, (int)p.splits) + chunks * n_kv_heads;
+  p.fits = p.groups < (1ll << 23) && p.merge_groups < (1ll << 24);  // 2^32 threads of a launch
   return p;
 }
 
 hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStream_t s) {
   if (a.B <= 0) return hipSuccess;
   if ((a.D != 64 && a.D != 128) || a.G < 1 || a.G > 16 || a.n_heads != a.G * a.n_kv_heads ||
-      (a.ldq % 8) || a.B > 65535 || p.splits < 1)
+      (a.ldq % 8) || a.B > 65535 || p.splits < 1 || !p.fits)
     return hipErrorInvalidValue;
-  const int chunks = a.acc_out ? (a.max_ctx + 1023) / 1024 : 0;
-  const int64_t tiles = ((int64_t)a.B * a.G + kTileRows - 1) / kTileRows;
-  const int64_t gx = (p.prefix_splits * tiles + a.B * p.own_splits) * a.n_kv_heads;
-  const int64_t gm = merge_groups(a.n_heads, (int)p.splits) + (int64_t)chunks * a.n_kv_heads;
-  if (gx >= (1ll << 23) || gm >= (1ll << 24)) return hipErrorInvalidValue;  // 2^32 threads of a launch
   a.lead_blocks = p.lead_blocks;
   a.prefix_tokens = p.prefix_tokens;
   a.prefix_splits = (int)p.prefix_splits;
@@ -786,7 +785,7 @@ hipError_t cache_attn(CacheAttnArgs a, const CacheAttnPlan& p, float* ws, hipStr
   a.scores = p.score_stride ? ws + p.scores : nullptr;
   a.score_stride = p.score_stride;
   const float sl = (float)(1.4426950408889634 / sqrt((double)a.D));
-  const dim3 grid((unsigned)gx), merge((unsigned)gm, a.B);
+  const dim3 grid((unsigned)p.groups), merge((unsigned)p.merge_groups, a.B);
   const auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;
     if (p.direct) {

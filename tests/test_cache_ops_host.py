@@ -122,3 +122,28 @@ def test_evictions_of_more_than_2_25_moves_are_refused():
     for keep, max_ctx in ((1 << 25, 1 << 26), (1 << 25, 1 << 30), ((1 << 30) - (1 << 25), 1 << 30), (2048, 1 << 30)):
         moves = min(keep, max_ctx - keep)
         assert hs.hs_k_kv_evict_ws(1, 1, keep, max_ctx) == 4 * (2 * moves + 1)
+
+
+def test_sizes_that_no_launch_takes_are_refused_with_their_workspace():
+    """What a call refuses for its size has no workspace size, and what has one is not refused for its size."""
+    refusing = 0
+    for B in (1, 64, 1024, 65535):
+        for nh, nkv in ((1, 1), (32, 8), (128, 128), (65536, 4096)):
+            for prefix, own in ((0, 1 << 20), (1 << 20, 300), (1 << 30, 1 << 30), (300, 5), (0, 1 << 30)):
+                for fn, size, args in ((hs.hs_k_attn_decode_shared, hs.hs_k_attn_decode_shared_ws, ATTN),
+                                       (hs.hs_k_attn_decode_weights, hs.hs_k_attn_decode_weights_ws, WEIGHTS | dict(acc_stride=1 << 30))):
+                    call = args | dict(B=B, n_heads=nh, n_kv_heads=nkv, ldq=nh * 128, ldo=nh * 128, prefix_len=prefix, max_ctx=own,
+                                       max_blocks=1 << 26, ws_bytes=0)
+                    try:
+                        need = size(B, nh, nkv, 128, prefix, own)
+                    except hs.HSError as e:
+                        assert e.code == hs.HS_EINVAL
+                        refused(hs.HS_EINVAL, fn, **(call | dict(ws_bytes=(1 << 64) - 1)))
+                        refusing += 1
+                    else:
+                        assert need > 0
+                        refused(hs.HS_ERANGE, fn, **call)
+    assert 20 < refusing < 140
+    size = hs.hs_k_attn_decode_shared_ws(64, 32, 8, 128, 0, 1 << 20)  # 2^22 workgroups: within a launch
+    assert size > 0
+    refused(hs.HS_EINVAL, hs.hs_k_attn_decode_shared_ws, 64, 32, 16, 128, 0, 1 << 20)  # 2^23
