@@ -158,7 +158,8 @@ hs_status hs_k_attn_decode_noalloc(const void* q, int64_t ldq, const void* pool,
  * that the matching _ws function gives (HS_ERANGE below it). ws need not be
  * cleared, and calls that may overlap in time need one each, replays of
  * captured calls too. Outputs overlap neither inputs nor each other but where it
- * says so. Buffers and the stream belong to the current device. B is at
+ * says so (HS_EINVAL; they may lie in the gaps of rows whose stride is the same;
+ * pools and rotary tables are not looked at). Buffers and the stream belong to the current device. B is at
  * most 65535, prefix_len and max_ctx at most 2^30, pool_blocks 2^27. A call of more
  * than 2^32 threads is refused, by its _ws function too: of attention over splits of
  * at least 128 tokens, a workgroup of 256 threads each per kv head, and of rotation, a thread per

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <string>
 
 #include "../../include/hs_kernel.h"
@@ -30,8 +31,49 @@ hs_status heads_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
   return HS_OK;
 }
 
+// An argument in memory: `rows` of `width` bytes, `stride` bytes apart (of one row: any). Pools and
+// rotary tables are left out of these checks: their sizes are bounds, which may be generous.
+typedef __int128 wide;  // (strides are the caller's)
+struct Array {
+  const char* name;
+  const void* at;
+  int64_t rows;
+  wide stride;
+  int64_t width;
+  bool written;
+};
+Array array(const char* name, const void* at, int64_t bytes, bool written = false) {
+  return Array{name, at, 1, 0, bytes, written};
+}
+
+// Whether two arrays share a byte: exact where their strides are alike, so that an array may lie
+// in the gaps of another's rows; else whether the ranges from first to last byte do.
+bool overlap(const Array& a, const Array& b) {
+  if (!a.at || !b.at || a.width <= 0 || b.width <= 0) return false;
+  const wide d = (wide)reinterpret_cast<uintptr_t>(b.at) - (wide)reinterpret_cast<uintptr_t>(a.at);
+  if (d >= (wide)(a.rows - 1) * a.stride + a.width || -d >= (wide)(b.rows - 1) * b.stride + b.width) return false;
+  if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
+  const wide s = a.rows > 1 ? a.stride : b.stride;
+  if (s <= 0) return true;
+  // row j of b lies d + (j - i) s behind row i of a: the first j - i that is more than -b.width
+  const wide x = -(wide)b.width - d;
+  wide m = (x >= 0 ? x / s : -((-x + s - 1) / s)) + 1;
+  m = std::max<wide>(m, -(wide)(a.rows - 1));
+  return m <= b.rows - 1 && d + m * s < a.width;
+}
+// HS_EINVAL if one that the call writes overlaps another (one that is read and written in place is
+// named once: its input is given without an address).
+hs_status apart(std::initializer_list<Array> arrays) {
+  for (auto a = arrays.begin(); a != arrays.end(); ++a)
+    for (auto b = a + 1; b != arrays.end(); ++b) {
+      if (!(a->written || b->written) || !overlap(*a, *b)) continue;
+      return fail(HS_EINVAL, std::string(a->name) + " and " + b->name + " overlap");
+    }
+  return HS_OK;
+}
+
 // Whether [a, a + na) and [b, b + nb) share a byte.
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+bool ranges_overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   const uint64_t x = reinterpret_cast<uint64_t>(a), y = reinterpret_cast<uint64_t>(b);
   return x < y + nb && y < x + na;
 }
@@ -121,9 +163,9 @@ extern "C" hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t*
     const int64_t nq = (int64_t)n_heads * head_dim, nk = (int64_t)n_kv_heads * head_dim;
     const uint64_t in = rows_bytes(T, ldqkv, nq + 2 * nk);
     const void* const keys = static_cast<const bf16_t*>(qkv) + nq;
-    if (overlap(qkv, in, q_out, rows_bytes(T, ldq, nq)) && (q_out != qkv || ldq != ldqkv))
+    if (ranges_overlap(qkv, in, q_out, rows_bytes(T, ldq, nq)) && (q_out != qkv || ldq != ldqkv))
       return fail(HS_EINVAL, "q_out overlaps qkv without being it");
-    if (k_out && overlap(qkv, in, k_out, rows_bytes(T, ldk, nk)) && (k_out != keys || ldk != ldqkv))
+    if (k_out && ranges_overlap(qkv, in, k_out, rows_bytes(T, ldk, nk)) && (k_out != keys || ldk != ldqkv))
       return fail(HS_EINVAL, "k_out overlaps qkv without being its keys");
     RopeKvAtArgs a{static_cast<const bf16_t*>(qkv), ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim,
                    layout == 1, static_cast<bf16_t*>(q_out), ldq, static_cast<bf16_t*>(k_out), k_out ? ldk : 0,
@@ -185,6 +227,18 @@ hs_status cache_attn_call(CacheAttnArgs a, bool weights, void* ws, uint64_t ws_b
   if (!p.fits) return fail(HS_EINVAL, "too many sequences, heads and tokens for a launch");
   const hs_status w = ws_ok(ws, ws_bytes, 4ull * p.floats);
   if (w != HS_OK) return w;
+  const int64_t width = 2ll * a.n_heads * a.D, rows = (int64_t)a.B * a.n_kv_heads, tokens = weights ? 4ll * a.max_ctx : 0;
+  const hs_status o = apart({{"q", a.q, a.B, 2 * (wide)a.ldq, width, false},
+                             {"out", a.out, a.B, 2 * (wide)a.ldo, width, true},
+                             array("prefix", a.prefix, 4 * (((int64_t)a.prefix_len + 15) / 16)),
+                             array("block_table", a.block_table, 4ll * a.B * a.max_blocks),
+                             array("ctx", a.ctx, 4ll * a.B),
+                             array("ws", ws, 4 * p.floats, true),
+                             {"acc", a.acc == a.acc_out ? nullptr : a.acc, rows, 4 * (wide)a.acc_stride, tokens, false},
+                             {"acc_out", a.acc_out, rows, 4 * (wide)a.acc_stride, tokens, true},
+                             {"pos", a.pos, rows, 4 * (wide)a.acc_stride, tokens, true},
+                             array("seen", a.pos ? a.seen : nullptr, 4ll * a.B)});
+  if (o != HS_OK) return o;
   return done(cache_attn(a, p, static_cast<float*>(ws), static_cast<hipStream_t>(stream)), "cache attention");
 }
 }  // namespace
@@ -308,6 +362,16 @@ extern "C" hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_
       return fail(HS_EINVAL, "pointers not aligned");
     const hs_status w = ws_ok(ws, ws_bytes, evict_bytes(B, n_kv_heads, keep, max_ctx));
     if (w != HS_OK) return w;
+    const int64_t rows = (int64_t)B * n_kv_heads, tokens = 4ll * max_ctx, kept = 4ll * std::min(keep, max_ctx);
+    const hs_status o = apart({array("block_table", block_table, 4ll * B * max_blocks),
+                               array("ctx", ctx, 4ll * B), array("seen", seen, 4ll * B),
+                               {"acc", acc == acc_out ? nullptr : acc, rows, 4 * (wide)stride, tokens, false},
+                               {"pos", pos == pos_out ? nullptr : pos, rows, 4 * (wide)stride, tokens, false},
+                               {"acc_out", acc_out, rows, 4 * (wide)out_stride, acc == acc_out ? tokens : kept, true},
+                               {"pos_out", pos_out, rows, 4 * (wide)out_stride, pos == pos_out ? tokens : kept, true},
+                               array("ctx_out", ctx_out, 4ll * B, true),
+                               array("ws", ws, (int64_t)evict_bytes(B, n_kv_heads, keep, max_ctx), true)});
+    if (o != HS_OK) return o;
     KvEvictArgs a{static_cast<bf16_t*>(pool), pool_blocks, block_table, ctx, seen, acc, pos, stride,
                   acc_out, pos_out, out_stride, ctx_out, keep, sinks, recent, B, n_kv_heads, head_dim,
                   max_blocks, max_ctx, static_cast<int32_t*>(ws), (int)evict_cap(keep, max_ctx), nullptr};

@@ -147,3 +147,56 @@ def test_sizes_that_no_launch_takes_are_refused_with_their_workspace():
     size = hs.hs_k_attn_decode_shared_ws(64, 32, 8, 128, 0, 1 << 20)  # 2^22 workgroups: within a launch
     assert size > 0
     refused(hs.HS_EINVAL, hs.hs_k_attn_decode_shared_ws, 64, 32, 16, 128, 0, 1 << 20)  # 2^23
+
+
+# arrays that lie apart, for the calls below: accepted ones end at the launch, which has no device here
+APART_ATTN = WEIGHTS | dict(q=P, out=2 * P, pool=3 * P, prefix=4 * P, block_table=5 * P, ctx=6 * P, acc=7 * P, acc_out=8 * P, pos=9 * P, seen=10 * P,
+                            ws=16 * P, ws_bytes=1 << 30)
+APART_EVICT = EVICT | dict(pool=20 * P, block_table=6 * P, ctx=7 * P, seen=8 * P, ws=16 * P, ws_bytes=1 << 30)
+
+
+@pytest.mark.parametrize("change", [
+    dict(out=P), dict(out=P + 4096), dict(acc_out=7 * P + 4), dict(acc_out=7 * P - 252), dict(acc_out=9 * P), dict(pos=7 * P), dict(seen=9 * P + 8),
+    dict(ctx=2 * P + 16), dict(ws=7 * P), dict(ws=P), dict(block_table=8 * P + 4), dict(prefix=2 * P)])
+def test_attention_arrays_that_overlap_are_refused(change):
+    refused(hs.HS_EINVAL, hs.hs_k_attn_decode_weights, **(APART_ATTN | change))
+
+
+@pytest.mark.parametrize("change", [dict(out=P), dict(out=P + 8192 - 16), dict(ctx=2 * P), dict(ws=5 * P), dict(block_table=2 * P + 4)])
+def test_shared_attention_arrays_that_overlap_are_refused(change):
+    a = {k: v for k, v in APART_ATTN.items() if k in ATTN}
+    refused(hs.HS_EINVAL, hs.hs_k_attn_decode_shared, **(a | change))
+
+
+@pytest.mark.parametrize("change", [
+    dict(acc_out=P + 4, out_stride=64), dict(acc_out=P - 4, out_stride=64), dict(acc_out=2 * P, out_stride=64), dict(pos_out=P, out_stride=64),
+    dict(acc_out=4 * P + 64), dict(ctx_out=8 * P), dict(ctx_out=7 * P + 4), dict(ctx_out=P), dict(ctx_out=16 * P), dict(ws=P), dict(ws=6 * P),
+    dict(acc_out=6 * P), dict(pos_out=2 * P + 256, out_stride=64)])
+def test_evictions_whose_arrays_overlap_are_refused(change):
+    refused(hs.HS_EINVAL, hs.hs_k_kv_evict, **(APART_EVICT | change))
+
+
+def accepted(fn, **kw):
+    """Whether a call passes the checks: where there is no device, it then fails at the launch."""
+    with pytest.raises(hs.HSError) as e:
+        fn(**kw)
+    assert e.value.code in (hs.HS_EINVAL, hs.HS_EHIP), e.value
+    return e.value.code == hs.HS_EHIP
+
+
+def without_device(f):
+    import torch
+    return pytest.mark.skipif(torch.cuda.is_available(), reason="would launch on memory that is not there")(f)
+
+
+@without_device
+def test_rows_are_refused_where_they_share_a_byte_and_only_there():
+    """Against the sets of bytes, for arrays in the gaps of another's rows: two strides alike, or one row."""
+    for B, nkv, most, stride in ((2, 2, 64, 150), (1, 1, 64, 64), (3, 1, 64, 70), (1, 5, 64, 200)):
+        base = APART_ATTN | dict(B=B, n_heads=4 * nkv, n_kv_heads=nkv, max_ctx=most, acc_stride=stride)
+        rows = B * nkv
+        mine = {7 * P + 4 * (r * stride + t) for r in range(rows) for t in range(most)}
+        for off in list(range(-2 * stride, 2 * stride, 7)) + [most, -most, most - 1, stride - most, stride - most + 1, rows * stride, -rows * stride]:
+            at = 7 * P + 4 * off
+            theirs = {at + 4 * (r * stride + t) for r in range(rows) for t in range(most)}
+            assert accepted(hs.hs_k_attn_decode_weights, **(base | dict(acc_out=at))) == (off == 0 or not mine & theirs), (B, nkv, stride, off)
