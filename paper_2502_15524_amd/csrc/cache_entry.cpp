@@ -72,14 +72,6 @@ hs_status apart(std::initializer_list<Array> arrays) {
   return HS_OK;
 }
 
-// Whether [a, a + na) and [b, b + nb) share a byte.
-bool ranges_overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  const uint64_t x = reinterpret_cast<uint64_t>(a), y = reinterpret_cast<uint64_t>(b);
-  return x < y + nb && y < x + na;
-}
-// Bytes from the first to the last element of rows of bf16.
-uint64_t rows_bytes(int64_t rows, int64_t ld, int64_t width) { return 2ull * ((rows - 1) * ld + width); }
-
 hs_status ws_ok(const void* ws, uint64_t bytes, uint64_t need) {
   if (bytes < need)
     return fail(HS_ERANGE, "workspace of " + std::to_string(bytes) + " bytes, needs " + std::to_string(need));
@@ -160,13 +152,17 @@ extern "C" hs_status hs_k_rope_kv(const void* qkv, int64_t ldqkv, const int32_t*
         !aligned(pos, 4) || !aligned(slot, 4))
       return fail(HS_EINVAL, "pointers or row strides not aligned");
     // in place, or apart
-    const int64_t nq = (int64_t)n_heads * head_dim, nk = (int64_t)n_kv_heads * head_dim;
-    const uint64_t in = rows_bytes(T, ldqkv, nq + 2 * nk);
-    const void* const keys = static_cast<const bf16_t*>(qkv) + nq;
-    if (ranges_overlap(qkv, in, q_out, rows_bytes(T, ldq, nq)) && (q_out != qkv || ldq != ldqkv))
-      return fail(HS_EINVAL, "q_out overlaps qkv without being it");
-    if (k_out && ranges_overlap(qkv, in, k_out, rows_bytes(T, ldk, nk)) && (k_out != keys || ldk != ldqkv))
-      return fail(HS_EINVAL, "k_out overlaps qkv without being its keys");
+    const int64_t nq = 2ll * n_heads * head_dim, nk = 2ll * n_kv_heads * head_dim, kv = nq + nk;
+    const wide ld = 2 * (wide)ldqkv;
+    const char* const x = static_cast<const char*>(qkv);
+    const bool q_in_place = q_out == qkv && ldq == ldqkv, k_in_place = k_out == x + nq && ldk == ldqkv;
+    const hs_status o = apart({{"the queries", q_in_place ? nullptr : x, T, ld, nq, false},
+                               {"the keys", k_in_place ? nullptr : x + nq, T, ld, nk, false},
+                               {"the values", x + kv, T, ld, nk, false},
+                               {"q_out", q_out, T, 2 * (wide)ldq, nq, true},
+                               {"k_out", k_out, T, 2 * (wide)ldk, nk, true},
+                               array("pos", pos, 4ll * T), array("slot", slot, 4ll * T)});
+    if (o != HS_OK) return o;
     RopeKvAtArgs a{static_cast<const bf16_t*>(qkv), ldqkv, pos, slot, cos_t, sin_t, max_pos, rot_dim,
                    layout == 1, static_cast<bf16_t*>(q_out), ldq, static_cast<bf16_t*>(k_out), k_out ? ldk : 0,
                    static_cast<bf16_t*>(pool), pool_blocks, T, n_heads, n_kv_heads, head_dim};

@@ -176,6 +176,14 @@ def test_evictions_whose_arrays_overlap_are_refused(change):
     refused(hs.HS_EINVAL, hs.hs_k_kv_evict, **(APART_EVICT | change))
 
 
+@pytest.mark.parametrize("change", [
+    dict(k_out=16 * P, ldk=1024), dict(k_out=16 * P + 8192 - 16, ldk=4096), dict(pos=16 * P + 64), dict(slot=16 * P), dict(q_out=P + 12288, ldq=48 * 128)])
+def test_rope_kv_outputs_that_overlap_are_refused(change):
+    a = dict(qkv=P, ldqkv=48 * 128, pos=2 * P, slot=3 * P, cos_t=4 * P, sin_t=5 * P, max_pos=64, rot_dim=128, layout="half", q_out=16 * P, ldq=32 * 128,
+             k_out=0, ldk=1024, pool=32 * P, pool_blocks=4, T=3, n_heads=32, n_kv_heads=8, head_dim=128) | change
+    refused(hs.HS_EINVAL, hs.hs_k_rope_kv, **a)
+
+
 def accepted(fn, **kw):
     """Whether a call passes the checks: where there is no device, it then fails at the launch."""
     with pytest.raises(hs.HSError) as e:
@@ -200,3 +208,14 @@ def test_rows_are_refused_where_they_share_a_byte_and_only_there():
             at = 7 * P + 4 * off
             theirs = {at + 4 * (r * stride + t) for r in range(rows) for t in range(most)}
             assert accepted(hs.hs_k_attn_decode_weights, **(base | dict(acc_out=at))) == (off == 0 or not mine & theirs), (B, nkv, stride, off)
+    for T, ld in ((3, 48 * 128 + 4096 + 64), (1, 48 * 128), (5, 48 * 128 + 1024)):
+        base = dict(qkv=P, ldqkv=ld, pos=2 * P, slot=3 * P, cos_t=4 * P, sin_t=5 * P, max_pos=64, rot_dim=128, layout="half", q_out=16 * P, ldq=ld,
+                    k_out=0, ldk=ld, pool=32 * P, pool_blocks=4, T=T, n_heads=32, n_kv_heads=8, head_dim=128)
+        unit = lambda at, n: {at // 16 + r * ld // 8 + t for r in range(T) for t in range(n // 8)}  # noqa: E731
+        whole, keys = unit(P, 48 * 128), unit(P + 8192, 1024)
+        for off in [0, 8, 4096, 5 * 1024, 6 * 1024, 6 * 1024 + 8, 48 * 128 + 64, -4096, -4096 - 8, ld * T, ld * (T - 1) + 48 * 128]:
+            got = accepted(hs.hs_k_rope_kv, **(base | dict(q_out=P + 2 * off)))
+            assert got == (off == 0 or not unit(P + 2 * off, 4096) & whole), (T, ld, off)
+            got = accepted(hs.hs_k_rope_kv, **(base | dict(k_out=P + 2 * off)))
+            assert got == (off == 4096 or not unit(P + 2 * off, 1024) & whole), (T, ld, off)
+        assert keys <= whole

@@ -3,9 +3,35 @@ import numpy as np
 import pytest
 
 from tests import gpu_util as G
-from tests.test_gpu_cache_ops import Cache, _hs, dev, host, workspace
+from tests.test_gpu_cache_ops import Cache, _hs, bf, dev, dev_bf, host, workspace
 
 pytestmark = pytest.mark.gpu
+
+
+def test_rope_kv_output_in_the_gaps_of_its_input():
+    """Queries and keys written behind the heads of the rows that they come from: the same bits as apart."""
+    torch = G.torch()
+    hs = _hs()
+    T, nh, nkv, d, rot, blocks = 33, 8, 2, 64, 32, 4
+    rng = np.random.default_rng(1)
+    width, nq, nk = (nh + 2 * nkv) * d, nh * d, nkv * d
+    ld = width + nq + nk + 24
+    x = bf(rng, (T, ld))
+    pos, slot = dev(rng.integers(0, 90, T).astype(np.int32)), dev(rng.permutation(blocks * 16)[:T].astype(np.int32))
+    ang = rng.uniform(0, 6.28, (90, rot // 2))
+    cos, sin = dev(np.cos(ang).astype(np.float32)), dev(np.sin(ang).astype(np.float32))
+    got = []
+    for gaps in (False, True):
+        qkv, pool = dev_bf(x), torch.zeros((blocks, 2, nkv, 16, d), dtype=torch.bfloat16, device="cuda")
+        q, k = torch.zeros((T, nq), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, nk), dtype=torch.bfloat16, device="cuda")
+        if gaps:
+            q, k = qkv[:, width:width + nq], qkv[:, width + nq:width + nq + nk]
+        hs.hs_k_rope_kv(qkv.data_ptr(), ld, pos.data_ptr(), slot.data_ptr(), cos.data_ptr(), sin.data_ptr(), 90, rot, "interleaved", q.data_ptr(),
+                        q.stride(0), k.data_ptr(), k.stride(0), pool.data_ptr(), blocks, T, nh, nkv, d, G.stream_ptr())
+        got.append([host(t.contiguous()) for t in (q, k, pool, qkv[:, :width], qkv[:, width + nq + nk:])])
+    assert np.abs(got[0][0]).max() > 0
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
 
 
 @pytest.mark.parametrize("lens,prefix", [([40, 7], 30), ([700, 1300], 900)])
