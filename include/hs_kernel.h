@@ -181,9 +181,9 @@ enum {
 typedef struct {
   int32_t kind;         /* HS_ROPE_* */
   int32_t original_ctx; /* BANDS and YARN: >= 1 */
-  double factor;        /* all but PLAIN: > 0 */
+  double factor;        /* all but PLAIN: > 0, w_i / factor finite */
   double low, high;     /* BANDS and YARN: 0 < low < high */
-  double magnitude;     /* cos and sin are multiplied by it (> 0) */
+  double magnitude;     /* cos and sin are multiplied by it (> 0, finite as float32) */
 } hs_rope_scaling;
 
 /* cos_t[p][i] = magnitude cos(p w_i'), sin_t[p][i] = magnitude sin(p w_i') for p <

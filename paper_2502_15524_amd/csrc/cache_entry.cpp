@@ -84,7 +84,8 @@ hs_status ws_ok(const void* ws, uint64_t bytes, uint64_t need) {
 hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, uint64_t* turns) {
   constexpr double kTwoPi = 6.283185307179586476925;
   if (c.kind < HS_ROPE_PLAIN || c.kind > HS_ROPE_YARN) return fail(HS_EINVAL, "unknown rotary scaling");
-  if (!(c.magnitude > 0) || !std::isfinite(c.magnitude)) return fail(HS_EINVAL, "magnitude must be positive");
+  if (!(c.magnitude > 0) || !std::isfinite((float)c.magnitude))
+    return fail(HS_EINVAL, "magnitude must be positive, and of float32");
   const bool banded = c.kind == HS_ROPE_BANDS || c.kind == HS_ROPE_YARN;
   if (c.kind != HS_ROPE_PLAIN && (!(c.factor > 0) || !std::isfinite(c.factor)))
     return fail(HS_EINVAL, "factor must be positive");
@@ -102,6 +103,7 @@ hs_status rope_turns(int32_t rot, double base, const hs_rope_scaling& c, uint64_
     if (c.kind == HS_ROPE_YARN) keep = 1.0 - (i - a) / std::max(b - a, 1e-3);
     keep = std::min(1.0, std::max(0.0, keep));
     if (keep < 1.0) w = (1.0 - keep) * w / c.factor + keep * w;
+    if (!std::isfinite(w)) return fail(HS_EINVAL, "factor too small");
     const double t = w / kTwoPi;
     turns[i] = static_cast<uint64_t>(ldexp(t - floor(t), 64));
   }

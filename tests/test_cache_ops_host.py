@@ -219,3 +219,11 @@ def test_rows_are_refused_where_they_share_a_byte_and_only_there():
             got = accepted(hs.hs_k_rope_kv, **(base | dict(k_out=P + 2 * off)))
             assert got == (off == 4096 or not unit(P + 2 * off, 1024) & whole), (T, ld, off)
         assert keys <= whole
+
+
+@pytest.mark.parametrize("scaling", [
+    hs.rope_scaling("linear", factor=1e-320), hs.rope_scaling("bands", factor=1e-310, original_ctx=10), hs.rope_scaling("linear", factor=2.0, magnitude=1e39),
+    hs.hs_rope_scaling(0, 0, 0.0, 0.0, 0.0, 1e300)])
+def test_scalings_whose_numbers_overflow_are_refused(scaling):
+    """Frequencies above float64 have no fraction of a turn, a magnitude above float32 makes NaN of a zero."""
+    refused(hs.HS_EINVAL, hs.hs_k_rope_tables, P, P, 64, 64, 10000.0, scaling)
