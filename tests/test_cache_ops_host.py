@@ -227,3 +227,11 @@ def test_rows_are_refused_where_they_share_a_byte_and_only_there():
 def test_scalings_whose_numbers_overflow_are_refused(scaling):
     """Frequencies above float64 have no fraction of a turn, a magnitude above float32 makes NaN of a zero."""
     refused(hs.HS_EINVAL, hs.hs_k_rope_tables, P, P, 64, 64, 10000.0, scaling)
+
+
+def test_the_forms_meant_by_the_long_attention_tests_are_taken():
+    """Each of them, if the rule that cuts a call changes: 2 to 16 steps of a prefix split, 8 to 32 blocks of an own one."""
+    from tests.test_gpu_cache_ops_forms import LONG, cut, splits
+    for lens, prefix, nh, nkv, d, prefix_tokens, own_blocks in LONG:
+        assert splits(hs, len(lens), nh, nkv, d, prefix, max(lens)) == cut(prefix, max(lens), prefix_tokens, own_blocks)
+    assert {x[5] for x in LONG} == {128, 192, 320, 704, 1024} and {x[6] for x in LONG} == {8, 16, 24, 32}
