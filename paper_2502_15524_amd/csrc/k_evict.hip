@@ -99,9 +99,10 @@ __device__ __forceinline__ void move_tokens(const KvEvictArgs& a, F pair, int j0
 template <int D, int K, bool MOVE>
 __global__ __launch_bounds__(kThreads, K == 0 || K == 16 ? 4 : 8) void kv_evict_select_kernel(KvEvictArgs a) {
   constexpr int R = K > 0 ? K : 1;
-  // of the first pass's histogram, by lane: most weights share a few exponents (four take fewer
-  // registers and reads, eight fewer turns at one address, 38.2 us for 38.8 at K = 16)
-  constexpr int kCopies = K == 16 ? 8 : 4;
+  // of the first pass's histogram, by lane: most weights share a few exponents. Eight copies are no
+  // faster in any form (MI355X, 8 -> 4: 64 rows of 11000 to 12000 tokens 38.0 -> 38.0 us, 512 of 12000 to 16000
+  // 297.2 -> 297.0, 256 of 2049 to 2176 12.4 -> 12.4, 960 of 4097 to 4224 41.2 -> 39.4)
+  constexpr int kCopies = 4;
   constexpr int kMoves = MOVE || K == 0 ? kMovesHere : 4096;  // listed in LDS
   __shared__ __attribute__((aligned(16))) uint32_t s_hist[256 * (kCopies + 3)];
   __shared__ __attribute__((aligned(16))) uint32_t s_wave[3][kWaves];
