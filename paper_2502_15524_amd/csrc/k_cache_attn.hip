@@ -16,9 +16,10 @@
 // are one split, whose workgroup writes output and weights without a second kernel.
 //
 // Bound by HBM: every cached key and value is read once. MI355X, merge included: 8B heads, 32
-// sequences of 64 to 512 tokens behind 8192 21.2 us (72 MB: 3.4 TB/s; in a kernel trace 19.4 and 3.9 for the
-// merge; the prefix's first copies take 3.7, its eight steps 8); 13B heads, 24 of up to 300 behind 2011
-// 27.5 us (4.3 TB/s); with weights, 24 of 512 to 4096 behind 1000 53.4 us (4.6 TB/s).
+// sequences of 64 to 512 tokens behind 8192 22.1 us (72 MB: 3.3 TB/s; in a kernel trace 20.9 and 3.9 for the
+// merge; a prefix of 2, 4, 8 and 16 steps to a workgroup with a token of their own takes 11.5, 13.8, 18.0 and
+// 25.8 there: 9 and 1.0 to 1.2 a step); 13B heads, 24 of up to 300 behind 2011 27.8 us (4.2 TB/s); with weights,
+// 24 of 512 to 4096 behind 1000 53.5 us (4.5 TB/s).
 #include "hs_device.h"
 #include "hs_kernels.h"
 
@@ -318,7 +319,7 @@ __device__ __forceinline__ void attn_split(const CacheAttnArgs& a, float scale_l
 // chunks of a row are XOR-swizzled so that the fragment reads and the transposing
 // reads of the values take different banks. Tiles of 64 rows, not 128 with 32 keys a
 // step: the same keys come from L2 for the second tile (8B heads, 32 sequences behind
-// 8192 tokens, MI355X: 26.4 us with 128 rows, 24.1 with 64).
+// 8192 tokens, MI355X, when this was chosen: 26.4 us with 128 rows, 24.1 with 64).
 template <int D>
 __device__ __forceinline__ int key_swz(int key) {
   return key & (D / 8 - 1);
@@ -443,8 +444,9 @@ __device__ __forceinline__ void attn_prefix(const CacheAttnArgs& a, float scale_
     f32x16_v s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
-    // one copy behind each product: in a row, the four waves' copies keep one another waiting (32 sequences
-    // behind 8192 tokens alone 20.7 -> 20.2 us)
+    // one copy behind each product: in a row, the four waves' copies keep one another waiting (MI355X, 32 sequences
+    // behind 8192 tokens, in a graph: 20.3 -> 20.0 us without caches of their own, 23.5 -> 23.2 with 64 to 512; 24 ragged ones
+    // behind 1000 53.3 and 53.4, 64 behind 4096 24.4 and 25.2)
     static_assert(2 * PER == D / 16, "as many copies as products");
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
@@ -631,9 +633,9 @@ __device__ __forceinline__ void merge_out(const CacheAttnArgs& a, int h, int b) 
   out[1] = pack2bf(o[2] * r, o[3] * r);
 }
 
-// The same for up to 32 splits, a wave alone: no exchange through LDS (with the main kernel, MI355X:
-// 8B heads, 64 sequences behind 4096 tokens 25.1 -> 23.0 us, 32 behind 8192 23.6 -> 23.0; 13B, 24 behind 2011
-// 28.9 -> 27.9).
+// The same for up to 32 splits, a wave alone: no exchange through LDS (with the main kernel, MI355X, in a graph:
+// 8B heads, 64 sequences behind 4096 tokens 26.9 -> 25.2 us, 32 behind 8192 24.0 -> 23.2; 13B, 24 behind 2011
+// 28.7 -> 28.2).
 template <int D>
 __device__ __forceinline__ void merge_out_wave(const CacheAttnArgs& a, int h, int b) {
   constexpr int LPR = D / 4, RPP = 64 / LPR, U = 32 / RPP;
@@ -729,28 +731,36 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t n_heads, int64_t n_kv_heads, in
   // Alone: a step of 256 slots at least as fast as splits and their merge at any batch; longer
   // ones where the workgroups fill the chip (128 and more for 3 and 4 steps), at two to a
   // CU in turn, or at one if each would read a prefix that the others have read. MI355X, in a graph, splits
-  // and merge -> alone: 3 sequences of 97 tokens, 4 heads 7.2 -> 3.4 us; 32 of 200, 8 kv heads 10.7 -> 6.1;
-  // 24 of 200, 40 heads 15.7 -> 14.4; 32 of 1000, 8 kv heads 23.9 -> 19.4; 28 of 400 behind 600 17.2 -> 13.5; 56 of
-  // 1000 38.4 -> 34.4. Left to the splits: 8 of 1000 10.6 (13.0 alone); 36 of 100 behind 900 13.2 (21.8), 48 of 400
-  // behind 600 19.2 (24.4).
+  // and merge -> alone: 3 sequences of 97 tokens, 4 heads 6.2 -> 3.5 us; 32 of 200, 8 kv heads 10.9 -> 7.4;
+  // 24 of 200, 40 heads 22.2 -> 18.1; 32 of 1000, 8 kv heads 27.5 -> 22.5; 28 of 400 behind 600 19.4 -> 14.1; 56 of
+  // 1000 43.7 -> 38.1. Left to the splits: 8 of 1000 11.5 (13.8 alone); 36 of 100 behind 900 13.5 (22.2), 48 of 400
+  // behind 600 21.7 (25.4).
   const int64_t groups = B * n_kv_heads;
   const bool prefixed = B > 1 && prefix_len > 0;
   p.direct = slots <= 256 || (groups <= (prefixed ? 256 : 512) && slots <= (groups < 128 ? 512 : kDirect));
   p.shared = !p.direct && prefixed;
   p.lead_blocks = p.shared ? 0 : (int)blocks;
+  // (Without a prefix, splits of 128 tokens: the step of a workgroup, none looped. In splits of 384 tokens of the
+  // looped form batches that fill the chip are faster and short ones slower: 24 of 512 to 4096 with weights 52.6 and
+  // 50.3 us, 64 of 1000 to 2000 73.7 and 68.0; one of 1100, 32 heads 10.0 and 11.5, 4 of 4000 18.3 and 19.7.)
   p.own_blocks = p.direct ? kDirect / 16 : 8;
   p.prefix_tokens = 0;
   p.prefix_splits = 0;
   if (p.shared) {
     // Every split costs the batch a partial result (520 bytes per query head at D = 128, written
     // and read), so a split is as long as leaves 256 workgroups to the prefix, one per CU, and to
-    // the sequences.
+    // the sequences. MI355X, in a graph, splits of 128, 256, 512 and 1024 tokens: 32 sequences of 64 to 512 behind 8192 38.0,
+    // 29.7, 22.5 and 28.5 us (512 taken), 64 of up to 200 behind 4096 36.8, 28.5, 23.8 and 27.4 (512), 16 of 500 behind
+    // 32000 70.1, 56.4, 47.5 and 41.6 (1000), 13B heads, 24 of up to 300 behind 2011 32.7, 28.8, 28.3 and 28.7 (320).
     const int64_t tiles = (rows + kTileRows - 1) / kTileRows;
     p.prefix_tokens = (int)std::min<int64_t>(
         kPrefixBlocks * 16, std::max<int64_t>(128, (prefix_len * n_kv_heads * tiles / 256 + 63) / 64 * 64));
     p.prefix_splits = (prefix_len + p.prefix_tokens - 1) / p.prefix_tokens;
-    // up to 512 of its slots in one split; longer ones in splits of 384 (of 256, 384, 512 and 1024 the
-    // best for ragged caches of 512 to 4096 tokens: 51.4, 49.0, 51.5 and 55.9 us for 24 of them)
+    // up to 512 of its slots in one split; longer ones in splits of 384. MI355X, in a graph, splits of 128, 256, 384, 512 and
+    // 1024 tokens: 24 of 512 to 4096 63.0, 57.7, 53.5, 56.6 and 60.3 us with weights, 57.9, 49.0, 45.6, 47.3 and 48.1 without; 64
+    // of 300 to 1000 52.8, 48.4, 42.7, 45.6 and 42.8; 16 of 600 to 1000 23.1, 22.4, 20.1, 21.3 and 23.2; 32 of 4096 124.5, 109.3, 106.7,
+    // 103.8 and 104.7; 7B heads, 4 of 512 to 4096 35.8, 31.4, 30.2, 29.7 and 34.3. Up to 512: 128 of 400 to 500 64.9,
+    // 56.3, 62.0, 53.5 and 53.4; 32 of 64 to 512 27.0, 24.3, 26.2, 22.4 and 22.5
     p.own_blocks = 8 * (int)std::min<int64_t>(max_ctx > 512 ? 3 : 4, std::max<int64_t>(1, groups * ((max_ctx + 127) / 128) / 256));
   }
   p.own_splits = (p.lead_blocks + (max_ctx + 15) / 16 + p.own_blocks - 1) / p.own_blocks;
