@@ -158,12 +158,12 @@ hs_status hs_k_attn_decode_noalloc(const void* q, int64_t ldq, const void* pool,
  * that the matching _ws function gives (HS_ERANGE below it). ws need not be
  * cleared, and calls that may overlap in time need one each, replays of
  * captured calls too. Outputs overlap neither inputs nor each other but where it
- * says so (HS_EINVAL; they may lie in the gaps of rows whose stride is the same;
- * pools and rotary tables are not looked at). Buffers and the stream belong to the current device. B is at
- * most 65535, prefix_len and max_ctx at most 2^30, pool_blocks 2^27. A call of more
- * than 2^32 threads is refused, by its _ws function too: of attention over splits of
- * at least 128 tokens, a workgroup of 256 threads each per kv head, and of rotation, a thread per
- * token and 16 elements of its heads.
+ * says so (HS_EINVAL; they may lie in the gaps of rows whose stride is the same; pools
+ * and rotary tables are not looked at). Buffers and the stream belong to the current
+ * device. B is at most 65535, prefix_len and max_ctx at most 2^30, pool_blocks 2^27. A
+ * call that needs 2^32 threads or more is refused, by its _ws function too: attention has
+ * 256 or 512 of them per kv head and split of a sequence (128 tokens or more), rotation one
+ * per token and 16 elements of its heads.
  * Results are deterministic. */
 
 /* How the angles of rotary positions are scaled. w_i = base^(-2 i / rot_dim) is
@@ -262,7 +262,8 @@ hs_status hs_k_attn_decode_weights(const void* q, int64_t ldq, const void* pool,
  * tokens are copied); they may be acc and pos themselves, with the same stride.
  * ctx_out[b] = min(ctx[b], keep), and may not be ctx. The sequences' own blocks are
  * distinct. stride >= max_ctx, out_stride >= min(keep, max_ctx); keep >= 1, sinks and
- * recent >= 0; at most 2^25 moves a row: min(keep, max_ctx - keep). A move from or to a block outside the pool is left out. */
+ * recent >= 0; min(keep, max_ctx - keep), the moves that a row can have, at most 2^25. A move
+ * from or to a block outside the pool is left out. */
 hs_status hs_k_kv_evict_ws(int32_t B, int32_t n_kv_heads, int32_t keep, int32_t max_ctx,
                            uint64_t* bytes);
 hs_status hs_k_kv_evict(void* pool, int32_t pool_blocks, const int32_t* block_table,
